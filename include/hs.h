@@ -174,7 +174,7 @@ HS_API int hs_tile_counts(const hs_shape* shape, const hs_policy* policy, int32_
 HS_API int hs_kv_bytes(const hs_shape* shape, const int32_t counts[5], size_t bytes[8]);
 
 /* Workspace bytes needed by each call.  [host, pure]
- *   op = 0 compress, 1 prefill (Lq = arg), 2 decode (n_splits = arg, 0 = auto), 3 re-compress
+ *   op = 0 compress, 1 prefill (Lq = arg), 2 decode (n_splits = arg, 0 = auto), 3 re-compress, 4 evict
  *   (op 1 needs none; op 3 only when the target ranks tiles: then 8 bytes per tile) */
 HS_API int hs_workspace_bytes(const hs_shape* shape, int op, int32_t arg, size_t* bytes);
 
@@ -353,6 +353,113 @@ HS_API int hs_decode_attn_tail(const hs_shape* shape, float scale, int32_t n_spl
 HS_API int hs_decode_attn_tail_rows(const hs_shape* shape, float scale, int32_t n_splits,
                              const void* Q, const hs_kv* kv, const void* tail_k, const void* tail_v,
                              const int32_t* tail_lens, void* O, float* LSE, void* workspace, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * A bounded cache: what stands in front of the cache (positions) and what keeps it small (tiles and tokens chosen by the attention
+ * they get).  Extensions of this library, in its own terms; the paper drops no tile of a cache in use.
+ * --------------------------------------------------------------------------------------------- */
+
+/* A tensor of D-channel vectors per (batch, head, token): first element and element strides of these three axes, the channels
+ * contiguous.  Strides of axes of size 1 are not looked at; the others are multiples of 8, data is 16-byte aligned. */
+typedef struct {
+  void* data;
+  int64_t batch, head, token;
+} hs_view;
+
+/* Rotary positions.  Pair i < rot_dim / 2 of a vector at position p is turned by the angle p theta_i and multiplied by `gain`:
+ *   (x, y) -> gain (x cos - y sin, x sin + y cos);
+ * the pair is channels (i, i + rot_dim / 2) (HS_ROPE_HALVES) or (2i, 2i + 1) (HS_ROPE_PAIRS); channels from rot_dim on are copied.
+ * theta_i = base^(-2i / rot_dim), for contexts longer than the trained one scaled:
+ *   HS_ROPE_LINEAR   theta_i / factor (positions are interpolated)
+ *   HS_ROPE_STRETCH  base times factor^(rot_dim / (rot_dim - 2)): the fastest pair keeps its angle, the slowest is divided by factor
+ *   HS_ROPE_BANDS    by the turns n_i = trained theta_i / 2 pi that a pair makes over the trained length: n_i >= high keeps theta_i,
+ *                    n_i <= low divides it by factor, between them s theta_i + (1 - s) theta_i / factor, s = (n_i - low) / (high - low)
+ *   HS_ROPE_RAMP     by the pair's number (YaRN, arXiv 2309.00071): theta_i up to pair a = floor(c(high)), theta_i / factor from pair
+ *                    b = ceil(c(low)), linear in i between, c(n) = rot_dim ln(trained / 2 pi n) / (2 ln base) the pair that makes n turns
+ *                    over the trained length, a >= 0, b <= rot_dim - 1 and at least a + 0.001; gain = 0.1 ln(factor) + 1 (1 for factor <= 1). */
+enum { HS_ROPE_HALVES = 0, HS_ROPE_PAIRS = 1 };
+enum { HS_ROPE_PLAIN = 0, HS_ROPE_LINEAR = 1, HS_ROPE_STRETCH = 2, HS_ROPE_BANDS = 3, HS_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t rot_dim;        /* channels that turn: a multiple of 16, 16 .. 128 */
+  int32_t layout;         /* HS_ROPE_HALVES or HS_ROPE_PAIRS */
+  int32_t scaling;        /* HS_ROPE_PLAIN .. HS_ROPE_RAMP */
+  int32_t trained;        /* BANDS and RAMP: tokens of the trained context */
+  double base;            /* > 1 */
+  double factor;          /* > 0; not read for PLAIN */
+  double low, high;       /* BANDS and RAMP: turns, 0 < low < high */
+} hs_rope_params;
+
+/* What hs_rope_plan makes of them, handed to the calls by value: turn[i] = theta_i / 2 pi in units of 2^-64 turns.  A position times
+ * turn[i], modulo 2^64, is the angle modulo one turn without rounding: exact for every position, also negative ones, which turn back. */
+typedef struct {
+  int32_t rot_dim, layout;
+  float gain;
+  int32_t reserved;       /* 0 */
+  uint64_t turn[64];
+} hs_rope;
+
+/* Fills *rope.  [host, pure] */
+HS_API int hs_rope_plan(const hs_rope_params* params, hs_rope* rope);
+
+/* Rotates the queries and keys of n tokens per batch row, as a projection leaves them, and puts queries, keys and values where attention
+ * and the cache take them from: the prompt's tensors, or the rows of the dense tail that the new tokens get.
+ *   q -> q_out  [B, n, Hq, D] -> [B, Hq, n, D]; both NULL: no queries in this call
+ *   k -> k_out, v -> v_out  [B, n, Hkv, D] -> [B, Hkv, n_rows, D]; all NULL, or v and v_out NULL, or none; values are copied
+ * (hs_view strides: any order of the axes.)  positions: device int32 [B, n], or NULL: token i stands at first_position + i in every row.
+ * rows: device int32 [B], or NULL: token i of batch row b goes to row rows[b] + i (first_row + i) of k_out and v_out; rows outside
+ * 0 .. n_rows - 1 are not written (a sequence that takes no part: rows[b] = -n or below).  Only B, Hq, Hkv, D and dtype of `shape` are
+ * looked at beyond its checks.  An output may be the input's memory vector for vector (in place), or not overlap any input or other output. */
+HS_API int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, const int32_t* positions, int32_t first_position,
+                const hs_view* q, const hs_view* q_out, const hs_view* k, const hs_view* k_out, const hs_view* v,
+                const hs_view* v_out, const int32_t* rows, int32_t first_row, int32_t n_rows, void* stream);
+
+/* Attention weight that the cache gathers: for every tile t (or token) of every (b, kv head)
+ *   mass_out = decay mass_in + sum over the group's Hq / Hkv heads, the Lq queries i and the tile's tokens j that i sees of
+ *              exp(scale q_i . k_j - LSE_i),
+ * the column sums of the softmax that prefill or decode attention over this cache computed, from the LSE that it returned (natural log).
+ * A query whose LSE is not finite (one that saw nothing; one the caller leaves out by setting its LSE to -inf) weighs nothing.
+ *   Q     [B, Hq, Lq, D], any Lq >= 1; query i stands at q_start + i and sees what hs_prefill_attn_at lets it see (0 <= q_start,
+ *         q_start + Lq <= L if causal, else q_start is not looked at)
+ *   LSE   fp32, element strides lse_strides[2] = {batch, head} (NULL: contiguous [B, Hq, Lq]), queries contiguous
+ *   mass  fp32 [B, Hkv, L / 64], or with per_token [B, Hkv, L]; mass_in NULL: zeros (as with decay 0, when it is not read); mass_out may be
+ *         mass_in.  Tiles that are SKIP get decay mass_in.
+ *   tail  the dense tail of a decode step (Lq == 1, causal 0): tail_k [B, Hkv, 64, D] contiguous or NULL, tail_len tokens valid
+ *         (tail_lens: device int32 [B] instead, clamped into 0 .. 64), counted to tile tail_tile (tail_tiles: device int32 [B] instead), the
+ *         one that the tail will be appended as; a tile outside 0 .. L / 64 - 1 drops the row's tail.
+ * workspace: hs_attn_mass_workspace_bytes bytes, 16-byte aligned (NULL where that is 0), not shared between two calls in flight; no
+ * initial content.  Sums are taken in fp32 in an order that depends on the arguments alone: equal calls give equal bits. */
+HS_API int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q,
+                 const float* LSE, const int64_t lse_strides[2], const hs_kv* kv, const void* tail_k, int32_t tail_len,
+                 const int32_t* tail_lens, int32_t tail_tile, const int32_t* tail_tiles, int per_token, float decay,
+                 const float* mass_in, float* mass_out, void* workspace, void* stream);
+
+/* Its workspace: 0 for one query, and where the tiles alone fill the GPU; at most 64 MiB.  [host, pure] */
+HS_API int hs_attn_mass_workspace_bytes(const hs_shape* shape, int32_t Lq, int causal, int per_token, size_t* bytes);
+
+/* Drops tiles from a packed cache in place: of the tiles a (b, kv head) row holds (not SKIP), without the first `first` and the last
+ * `last` of them, the held - keep of lowest mass become SKIP in K and V (ties and equal zeros: the lower tile first; NaN is below everything).
+ * mass: device fp32 [B, Hkv, L / 64].  keep >= 1, or keeps: device int32 [B, Hkv] instead (below 1 counts as 1).  A row that holds no
+ * more than `keep` tiles, or only protected ones, is left as it is.
+ * Nothing is copied but what has to move: the used slots of a pool are 0 .. n - 1 again afterwards, because the remaining tiles whose slots
+ * are n or above move, in ascending order, into the freed slots below n, in ascending order (at most as many moves as dropped tiles),
+ * so hs_append_tile goes on from there.  Slots from n on keep their bytes.  Every held tile's slots have to be distinct and 0 .. n - 1
+ * in their pool, as all calls of this library leave them.  kv->uniform must be 0.  L / 64 <= 65536.
+ * workspace: hs_workspace_bytes(op 4), 4-byte aligned, not shared between two calls in flight; no initial content. */
+HS_API int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* mass, int32_t keep, const int32_t* keeps, int32_t first,
+                   int32_t last, void* workspace, void* stream);
+
+/* Chooses the tokens of a prompt that go into a cache: of the n_tokens of a (b, kv head) row (lens: device int32 [B], or NULL, the
+ * tokens of a batch row that are valid, clamped into 0 .. n_tokens) the first `first`, the last `last` and of the others those of
+ * largest weight, `keep` in all (ties and equal zeros: the lower token first; NaN is below everything), in order of position.
+ *   K, V      [B, Hkv, n_tokens, D] -> K_out, V_out [B, Hkv, keep, D] contiguous
+ *   weight    device fp32, element strides weight_strides[2] = {batch, head} (NULL: contiguous [B, Hkv, n_tokens]), tokens contiguous
+ *   index     device int32 [B, Hkv, keep]: the tokens kept
+ * A row of fewer than `keep` tokens keeps them all; the rest of its outputs is 0 and its indices -1.  keep >= first + last,
+ * keep >= 1, n_tokens <= 2^24.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  No workspace; outputs
+ * overlap neither inputs nor each other. */
+HS_API int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,
+                   const int64_t weight_strides[2], const int32_t* lens, int32_t keep, int32_t first, int32_t last, void* K_out,
+                   void* V_out, int32_t* index, void* stream);
 
 #ifdef __cplusplus
 }

@@ -44,6 +44,21 @@ class HsKV(C.Structure):
                 ("cap_sparse_v", C.c_int32), ("uniform", C.c_int32)]
 
 
+class HsView(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class HsRopeParams(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("trained", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class HsRope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("gain", C.c_float), ("reserved", C.c_int32), ("turn", C.c_uint64 * 64)]
+
+
+_VIEW = C.POINTER(HsView)
+
 EXPORTS = {
     "hs_version": (C.c_int, []),
     "hs_strerror": (C.c_char_p, [C.c_int]),
@@ -89,6 +104,17 @@ EXPORTS = {
                                  C.POINTER(C.c_int64), C.POINTER(HsKV), C.c_void_p, C.c_void_p]),
     "hs_decode_attn_tail": (C.c_int, [C.POINTER(HsShape), C.c_float, C.c_int32, C.c_void_p, C.POINTER(HsKV), C.c_void_p,
                                       C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hs_rope_plan": (C.c_int, [C.POINTER(HsRopeParams), C.POINTER(HsRope)]),
+    "hs_rope_qkv": (C.c_int, [C.POINTER(HsShape), C.POINTER(HsRope), C.c_int32, C.c_void_p, C.c_int32, _VIEW, _VIEW, _VIEW, _VIEW, _VIEW,
+                              _VIEW, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
+    "hs_attn_mass": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int32, C.c_float, C.c_int, _VIEW, C.c_void_p, C.POINTER(C.c_int64),
+                               C.POINTER(HsKV), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int, C.c_float,
+                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hs_attn_mass_workspace_bytes": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "hs_evict_tiles": (C.c_int, [C.POINTER(HsShape), C.POINTER(HsKV), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+                                 C.c_void_p, C.c_void_p]),
+    "hs_keep_tokens": (C.c_int, [C.POINTER(HsShape), C.c_int32, _VIEW, _VIEW, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int32,
+                                 C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "hs_decode_attn_phases": (C.c_int, [C.POINTER(HsShape), C.c_float, C.c_int32, C.c_void_p, C.POINTER(HsKV),
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
 }
@@ -113,11 +139,12 @@ def lib():
 # entry points that the native part calls, in the order it has them
 _NATIVE_ENTRIES = ("hs_kv_bytes", "hs_workspace_bytes", "hs_decode_auto_splits", "hs_decode_attn", "hs_decode_attn_static",
                    "hs_decode_attn_tail", "hs_decode_attn_tail_rows", "hs_prefill_plan", "hs_prefill_attn_ws",
-                   "hs_append_tiles", "hs_append_tile_rows", "hs_tile_counts", "hs_compress_kv", "hs_recompress_kv")
+                   "hs_append_tiles", "hs_append_tile_rows", "hs_tile_counts", "hs_compress_kv", "hs_recompress_kv", "hs_rope_qkv", "hs_attn_mass",
+                   "hs_attn_mass_workspace_bytes", "hs_evict_tiles", "hs_keep_tokens")
 
 
 # what calls it
-_NATIVE_CALLS = ("decode", "decode_static", "prefill", "append", "pools", "compress", "recompress")
+_NATIVE_CALLS = ("decode", "decode_static", "prefill", "append", "pools", "compress", "recompress", "rope", "mass", "evict", "keep")
 
 
 def _load_native(L):
@@ -133,7 +160,7 @@ def _load_native(L):
         warnings.warn(f"the binding runs without its native part ({why}): small calls take longer; `python -m paper_2604_16864_amd.build` "
                       "builds it", RuntimeWarning, stacklevel=3)
         return types.SimpleNamespace(**{name: lambda *args: None for name in _NATIVE_CALLS})
-    _hs_torch.bind(tuple(C.cast(getattr(L, name), C.c_void_p).value for name in _NATIVE_ENTRIES), HsShape, HsPolicy, PackedKV)
+    _hs_torch.bind(tuple(C.cast(getattr(L, name), C.c_void_p).value for name in _NATIVE_ENTRIES), HsShape, HsPolicy, PackedKV, HsRope)
     return _hs_torch
 
 
@@ -566,6 +593,171 @@ def decode_attn_static(shape, Q, kv, scale=0.0, n_splits=0, out=None, lse=None):
     _check(lib().hs_decode_attn_static(C.byref(shape), float(scale), int(n_splits), _ptr(Q), C.byref(kvs), _ptr(out),
                                        _ptr(lse), _stream()))
     return out, lse
+
+
+# ---- a bounded cache: rotary positions, attention mass, eviction of tiles, choice of tokens ----
+
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_STRETCH, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
+OP_EVICT = 4          # hs_workspace_bytes: scratch of evict_tiles
+
+
+def make_rope(rot_dim=HEAD_DIM, layout=ROPE_HALVES, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, low=0.0, high=0.0, trained=0):
+    """The angles of rope_qkv (hs_rope_plan): rot_dim channels of a head turn (a multiple of 16), channel i with i + rot_dim / 2 (ROPE_HALVES) or
+    2i with 2i + 1 (ROPE_PAIRS).  scaling stretches the context by `factor`: ROPE_LINEAR, ROPE_STRETCH (of the base), ROPE_BANDS and ROPE_RAMP
+    (by the turns a pair makes over the `trained` tokens: more than `high` keep their angle, fewer than `low` are divided)."""
+    params = HsRopeParams(int(rot_dim), int(layout), int(scaling), int(trained), float(base), float(factor), float(low), float(high))
+    rope = HsRope()
+    _check(lib().hs_rope_plan(C.byref(params), C.byref(rope)))
+    return rope
+
+
+def _here(*tensors):
+    """The calls below launch on the current stream of the current device: tensors of another one are refused."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise HsError(f"a tensor on {t.device}: the call runs on the current device")
+
+
+def _view(t, head, token):
+    assert t.stride(3) == 1
+    return HsView(t.data_ptr(), t.stride(0), t.stride(head), t.stride(token))
+
+
+def _int32(t, sizes):
+    assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == sizes
+    return t.data_ptr()
+
+
+def rope_qkv(shape, rope, q=None, k=None, v=None, positions=0, q_out=None, k_out=None, v_out=None, rows=0):
+    """Rotates the queries q [B, n, Hq, D] and keys k [B, n, Hkv, D] of n new tokens per sequence (views of a projection, last dim contiguous)
+    and puts them, and the values v, where attention and the cache take them from: q_out [B, Hq, n, D], k_out and v_out
+    [B, Hkv, R, D] (tensors of the prompt, or the dense tail with R = 64).  Any of q, (k), (k, v) may be left out.
+    positions: of the first token (an int), or int32 device tensor [B, n].  rows: row of k_out and v_out that the first token gets, an
+    int or int32 device tensor [B]; rows outside k_out are not written.  Returns (q_out, k_out, v_out), made where not given."""
+    r = _fast().rope(shape, rope, q, k, v, positions, q_out, k_out, v_out, rows)
+    if r is not None:
+        return _done(r)
+    some = q if q is not None else k
+    assert some is not None and (v is None or k is not None)
+    _here(q, k, v, q_out, k_out, v_out)
+    B, n = some.shape[0], some.shape[1]
+    for t, heads in ((q, shape.Hq), (k, shape.Hkv), (v, shape.Hkv)):
+        assert t is None or (t.dtype == torch_dtype(shape) and tuple(t.shape) == (shape.B, n, heads, shape.D))
+    if q is not None and q_out is None:
+        q_out = q.new_empty((B, shape.Hq, n, shape.D))
+    if k is not None and k_out is None:
+        k_out = k.new_empty((B, shape.Hkv, n, shape.D) if v_out is None else v_out.shape)
+    if v is not None and v_out is None:
+        v_out = v.new_empty(k_out.shape)
+    assert (q is not None or q_out is None) and (k is not None or k_out is None) and (v is not None or v_out is None)
+    assert q_out is None or (q_out.dtype == q.dtype and tuple(q_out.shape) == (B, shape.Hq, n, shape.D))
+    n_rows = 0 if k_out is None else k_out.shape[2]
+    for t in (k_out, v_out):
+        assert t is None or (t.dtype == k.dtype and tuple(t.shape) == (B, shape.Hkv, n_rows, shape.D))
+    views = [None if t is None else _view(t, h, i) for t, h, i in ((q, 2, 1), (q_out, 1, 2), (k, 2, 1), (k_out, 1, 2), (v, 2, 1), (v_out, 1, 2))]
+    pos, first = (_int32(positions, (B, n)), 0) if torch.is_tensor(positions) else (None, int(positions))
+    at, row0 = (_int32(rows, (B,)), 0) if torch.is_tensor(rows) else (None, int(rows))
+    _here(*(t for t in (positions, rows) if torch.is_tensor(t)))
+    _check(lib().hs_rope_qkv(C.byref(shape), C.byref(rope), n, pos, first, *(None if x is None else C.byref(x) for x in views), at, row0,
+                             n_rows, _stream()))
+    return q_out, k_out, v_out
+
+
+def attn_mass(shape, Q, lse, kv, mass=None, out=None, per_token=False, decay=1.0, causal=None, scale=0.0, q_start=None, tail_k=None,
+              tail_len=None, tail_tile=None, workspace=None):
+    """Attention weight that the tiles (or tokens) of the cache gather: decay * mass + the column sums of the softmax of the queries Q
+    [B, Hq, Lq, D] (or [B, Hq, D]: one per head) whose log-sum-exps lse [B, Hq(, Lq)] prefill_attn or decode_attn returned, summed over the
+    query heads of a kv head.  Views are taken (the last queries of a prompt: Q[:, :, -n:], lse[:, :, -n:]); a query whose lse is not
+    finite weighs nothing.  mass: fp32 [B, Hkv, L / 64] (per_token: [B, Hkv, L]) or None; out: where the sum goes (default: into mass,
+    or a new tensor).  causal (default: for queries with a token axis), q_start: as for prefill_attn.  tail_k [B, Hkv, 64, D], tail_len (int
+    or int32 device tensor [B]): the dense tail of a decode step, counted to tile tail_tile (int or int32 device tensor [B])."""
+    r = _fast().mass(shape, Q, lse, kv, mass, out, per_token, decay, causal, scale, q_start, tail_k, tail_len, tail_tile, workspace)
+    if r is not None:
+        return _done(r)
+    if causal is None:
+        causal = Q.dim() == 4
+    if Q.dim() == 3:
+        Q, lse = Q.unsqueeze(2), lse.unsqueeze(2)
+    _here(Q, lse, mass, out, tail_k, workspace, kv.k_map)
+    Lq, T = Q.shape[2], shape.L // TILE
+    assert Q.dtype == torch_dtype(shape) and tuple(Q.shape) == (shape.B, shape.Hq, Lq, shape.D)
+    assert lse.dtype == torch.float32 and tuple(lse.shape) == (shape.B, shape.Hq, Lq) and (Lq == 1 or lse.stride(2) == 1)
+    sizes = (shape.B, shape.Hkv, shape.L if per_token else T)
+    if out is None:
+        out = Q.new_empty(sizes, dtype=torch.float32) if mass is None else mass
+    for t in (mass, out):
+        assert t is None or (t.dtype == torch.float32 and tuple(t.shape) == sizes and t.is_contiguous())
+    n_tail, lens, n_tile, tiles = 0, None, 0, None
+    if tail_k is not None:
+        assert tail_len is not None and tail_tile is not None
+        assert tail_k.dtype == Q.dtype and tail_k.is_contiguous() and tuple(tail_k.shape) == (shape.B, shape.Hkv, TILE, shape.D)
+        n_tail, lens = (0, _int32(tail_len, (shape.B,))) if torch.is_tensor(tail_len) else (int(tail_len), None)
+        n_tile, tiles = (0, _int32(tail_tile, (shape.B,))) if torch.is_tensor(tail_tile) else (int(tail_tile), None)
+        _here(*(t for t in (tail_len, tail_tile) if torch.is_tensor(t)))
+    need = C.c_size_t(0)
+    _check(lib().hs_attn_mass_workspace_bytes(C.byref(shape), Lq, int(bool(causal)), int(bool(per_token)), C.byref(need)))
+    if workspace is None:
+        workspace = _workspace(need.value, Q.device) if need.value else None
+    assert workspace is None or workspace.nbytes >= need.value
+    at = shape.L - Lq if q_start is None else int(q_start)
+    kvs = kv.struct()
+    _check(lib().hs_attn_mass(C.byref(shape), Lq, at if causal else 0, float(scale), int(bool(causal)), C.byref(_view(Q, 1, 2)), _ptr(lse),
+                              (C.c_int64 * 2)(lse.stride(0), lse.stride(1)), C.byref(kvs), _ptr(tail_k), n_tail, lens, n_tile, tiles,
+                              int(bool(per_token)), float(decay), _ptr(mass), _ptr(out), _ptr(workspace), _stream()))
+    return out
+
+
+def attn_mass_workspace_bytes(shape, Lq, causal=True, per_token=False):
+    """Scratch that attn_mass takes for this call."""
+    need = C.c_size_t(0)
+    _check(lib().hs_attn_mass_workspace_bytes(C.byref(shape), int(Lq), int(bool(causal)), int(bool(per_token)), C.byref(need)))
+    return need.value
+
+
+def evict_tiles(shape, kv, mass, keep, first=0, last=0, workspace=None):
+    """Drops tiles of the packed cache `kv` in place until each (b, kv head) row holds `keep` (an int, or int32 device tensor [B, Hkv]): those of
+    lowest mass (fp32 [B, Hkv, L / 64], see attn_mass) but for the row's first `first` and last `last` held tiles.  Few tiles move: the
+    remaining ones of the highest slots fill the freed ones.  kv is no uniform cache afterwards (kv.uniform becomes 0)."""
+    if _done(_fast().evict(shape, kv, mass, keep, first, last, workspace)) is not None:
+        kv.uniform = 0
+        return
+    _here(mass, workspace, kv.k_map)
+    assert mass.dtype == torch.float32 and mass.is_contiguous() and tuple(mass.shape) == (shape.B, shape.Hkv, shape.L // TILE)
+    n, per_row = (0, _int32(keep, (shape.B, shape.Hkv))) if torch.is_tensor(keep) else (int(keep), None)
+    if torch.is_tensor(keep):
+        _here(keep)
+    need = workspace_bytes(shape, OP_EVICT)
+    if workspace is None:
+        workspace = _workspace(need, mass.device)
+    assert workspace.nbytes >= need
+    kvs = kv.struct()
+    kvs.uniform = 0
+    _check(lib().hs_evict_tiles(C.byref(shape), C.byref(kvs), _ptr(mass), n, per_row, int(first), int(last), _ptr(workspace), _stream()))
+    kv.uniform = 0
+
+
+def keep_tokens(shape, K, V, weight, keep, first=0, last=0, lens=None):
+    """The `keep` tokens of every (b, kv head) row of K, V [B, Hkv, n, D] that go into a cache: the first `first`, the last `last` and of the
+    others those of largest weight (fp32 [B, Hkv, n], see attn_mass with per_token), in order of position.  lens: int32 device tensor [B], the
+    valid tokens of each sequence.  Returns (K_out, V_out [B, Hkv, keep, D], index int32 [B, Hkv, keep]); a row of fewer tokens
+    ends in zeros and indices of -1."""
+    r = _fast().keep(shape, K, V, weight, keep, first, last, lens)
+    if r is not None:
+        return _done(r)
+    _here(K, V, weight, lens)
+    n, keep = K.shape[2], int(keep)
+    assert K.dtype == torch_dtype(shape) and V.dtype == K.dtype and K.shape == V.shape and tuple(K.shape) == (shape.B, shape.Hkv, n, shape.D)
+    assert weight.dtype == torch.float32 and tuple(weight.shape) == (shape.B, shape.Hkv, n) and (n == 1 or weight.stride(2) == 1)
+    at = None if lens is None else _int32(lens, (shape.B,))
+    if keep < 1:
+        raise HsError("keep_tokens: at least one token is kept")
+    K_out = K.new_empty((shape.B, shape.Hkv, keep, shape.D))
+    V_out, index = torch.empty_like(K_out), torch.empty(K_out.shape[:3], dtype=torch.int32, device=K.device)
+    _check(lib().hs_keep_tokens(C.byref(shape), n, C.byref(_view(K, 1, 2)), C.byref(_view(V, 1, 2)), _ptr(weight),
+                                (C.c_int64 * 2)(weight.stride(0), weight.stride(1)), at, keep, int(first), int(last), _ptr(K_out), _ptr(V_out),
+                                _ptr(index), _stream()))
+    return K_out, V_out, index
 
 
 def bits_to_bf16_tensor(bits, device="cuda", dtype=torch.bfloat16):

@@ -233,6 +233,7 @@ int hs_workspace_bytes(const hs_shape* shape, int op, int32_t arg, size_t* bytes
       return HS_OK;
     }
     case 3: *bytes = 2 * rows * T * sizeof(int32_t); return HS_OK;
+    case 4: *bytes = hs_evict_ws_ints((int64_t)rows, (int)T) * sizeof(int32_t); return HS_OK;
     default: return HS_EINVAL;
   }
 }
@@ -565,6 +566,184 @@ int hs_decode_attn_tail_rows(const hs_shape* shape, float scale, int32_t n_split
   if (tail_k == nullptr || tail_v == nullptr || tail_lens == nullptr) return HS_EINVAL;
   if (((uintptr_t)tail_k | (uintptr_t)tail_v) & 15u) return HS_EINVAL;
   return decode_common(shape, scale, n_splits, Q, kv, tail_k, tail_v, 0, tail_lens, O, LSE, workspace, stream, 3);
+}
+
+}  // extern "C"
+
+// -------- rotary positions, attention mass, eviction, token choice --------
+namespace {
+
+// A view of [n_b, n_h, n_t] vectors.  Strides of axes of size 1 are replaced by 0: they are not looked at.
+int view_of(const hs_view* v, int64_t n_b, int64_t n_h, int64_t n_t, bool out, hs_vec_view* to) {
+  if (v->data == nullptr || ((uintptr_t)v->data & 15u)) return HS_EINVAL;
+  *to = hs_vec_view{(uint16_t*)v->data, n_b > 1 ? v->batch : 0, n_h > 1 ? v->head : 0, n_t > 1 ? v->token : 0};
+  if (to->sb < 0 || to->sh < 0 || to->st < 0 || ((to->sb | to->sh | to->st) & 7)) return HS_EINVAL;
+  // two vectors of an output must not share memory
+  if (out && ((n_b > 1 && to->sb < HS_D) || (n_h > 1 && to->sh < HS_D) || (n_t > 1 && to->st < HS_D))) return HS_EINVAL;
+  return HS_OK;
+}
+
+double rope_pair_with(const hs_rope_params* p, double turns) {
+  return p->rot_dim * log(p->trained / (turns * 2.0 * M_PI)) / (2.0 * log(p->base));
+}
+
+}  // namespace
+
+extern "C" {
+
+int hs_rope_plan(const hs_rope_params* p, hs_rope* rope) {
+  if (p == nullptr || rope == nullptr) return HS_EINVAL;
+  if (p->rot_dim < 16 || p->rot_dim > HS_D || p->rot_dim % 16 != 0) return HS_EUNSUPPORTED;
+  if (p->layout != HS_ROPE_HALVES && p->layout != HS_ROPE_PAIRS) return HS_EINVAL;
+  if (p->scaling < HS_ROPE_PLAIN || p->scaling > HS_ROPE_RAMP) return HS_EINVAL;
+  if (!(p->base > 1.0) || !(p->base < INFINITY)) return HS_EINVAL;
+  const double f = p->scaling == HS_ROPE_PLAIN ? 1.0 : p->factor;
+  if (!(f > 0.0) || !(f < INFINITY)) return HS_EINVAL;
+  const bool by_turns = p->scaling == HS_ROPE_BANDS || p->scaling == HS_ROPE_RAMP;
+  if (by_turns && (p->trained < 1 || !(p->low > 0.0) || !(p->high > p->low) || !(p->high < INFINITY))) return HS_EINVAL;
+  memset(rope, 0, sizeof(*rope));
+  rope->rot_dim = p->rot_dim;
+  rope->layout = p->layout;
+  rope->gain = 1.f;
+  const double r = p->rot_dim;
+  const double base = p->scaling == HS_ROPE_STRETCH ? p->base * pow(f, r / (r - 2.0)) : p->base;
+  double a = 0.0, b = 0.0;
+  if (p->scaling == HS_ROPE_RAMP) {
+    a = fmax(0.0, floor(rope_pair_with(p, p->high)));
+    b = fmin(r - 1.0, ceil(rope_pair_with(p, p->low)));
+    b = fmax(b, a + 0.001);
+    if (f > 1.0) rope->gain = (float)(0.1 * log(f) + 1.0);
+  }
+  for (int i = 0; i < p->rot_dim / 2; i++) {
+    double theta = pow(base, -2.0 * i / r);
+    double keeps = 1.0;  // share of theta, the rest of theta / factor
+    if (p->scaling == HS_ROPE_LINEAR) keeps = 0.0;
+    if (p->scaling == HS_ROPE_BANDS) keeps = (p->trained * theta / (2.0 * M_PI) - p->low) / (p->high - p->low);
+    if (p->scaling == HS_ROPE_RAMP) keeps = 1.0 - (i - a) / (b - a);
+    keeps = fmin(1.0, fmax(0.0, keeps));
+    theta = keeps * theta + (1.0 - keeps) * (theta / f);
+    const double turns = theta / (2.0 * M_PI), part = turns - floor(turns);  // whole turns of a step do not matter
+    const double units = ldexp(part, 64) + 0.5;
+    rope->turn[i] = units >= 18446744073709551615.0 ? 0 : (uint64_t)units;
+  }
+  return HS_OK;
+}
+
+int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, const int32_t* positions, int32_t first_position,
+                const hs_view* q, const hs_view* q_out, const hs_view* k, const hs_view* k_out, const hs_view* v,
+                const hs_view* v_out, const int32_t* rows, int32_t first_row, int32_t n_rows, void* stream) {
+  const int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  if (rope == nullptr || rope->rot_dim < 16 || rope->rot_dim > HS_D || rope->rot_dim % 16 != 0 ||
+      (rope->layout != HS_ROPE_HALVES && rope->layout != HS_ROPE_PAIRS))
+    return HS_EINVAL;
+  if (n < 1 || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr)) return HS_EINVAL;
+  if ((q == nullptr && k == nullptr) || (v != nullptr && k == nullptr)) return HS_EINVAL;
+  if ((int64_t)shape->B * n > INT32_MAX) return HS_EUNSUPPORTED;
+  if (k != nullptr && n_rows < 1) return HS_EINVAL;
+  hs_rope_args a = {};
+  a.rope = *rope;
+  int bad = HS_OK;
+  if (q != nullptr) {
+    if (bad == HS_OK) bad = view_of(q, shape->B, shape->Hq, n, false, &a.q);
+    if (bad == HS_OK) bad = view_of(q_out, shape->B, shape->Hq, n, true, &a.qo);
+  }
+  if (k != nullptr) {
+    if (bad == HS_OK) bad = view_of(k, shape->B, shape->Hkv, n, false, &a.k);
+    if (bad == HS_OK) bad = view_of(k_out, shape->B, shape->Hkv, n_rows, true, &a.ko);
+  }
+  if (v != nullptr) {
+    if (bad == HS_OK) bad = view_of(v, shape->B, shape->Hkv, n, false, &a.v);
+    if (bad == HS_OK) bad = view_of(v_out, shape->B, shape->Hkv, n_rows, true, &a.vo);
+  }
+  if (bad != HS_OK) return bad;
+  a.positions = positions; a.rows = rows;
+  a.n = n; a.first_position = first_position; a.first_row = first_row; a.n_rows = n_rows;
+  a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv;
+  const hipError_t e = hs_launch_rope(a, shape->dtype, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_attn_mass_workspace_bytes(const hs_shape* shape, int32_t Lq, int causal, int per_token, size_t* bytes) {
+  const int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  if (Lq < 1 || bytes == nullptr) return HS_EINVAL;
+  const int T = shape->L / HS_BT;
+  const int n = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, T, Lq, causal != 0, per_token != 0);
+  *bytes = n > 1 ? (size_t)n * shape->B * shape->Hkv * T * (per_token != 0 ? HS_BT : 1) * sizeof(float) : 0;
+  return HS_OK;
+}
+
+int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q,
+                 const float* LSE, const int64_t lse_strides[2], const hs_kv* kv, const void* tail_k, int32_t tail_len,
+                 const int32_t* tail_lens, int32_t tail_tile, const int32_t* tail_tiles, int per_token, float decay,
+                 const float* mass_in, float* mass_out, void* workspace, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  rc = check_kv(shape, kv);
+  if (rc != HS_OK) return rc;
+  if (Lq < 1 || Q == nullptr || LSE == nullptr || mass_out == nullptr) return HS_EINVAL;
+  if (((uintptr_t)LSE | (uintptr_t)mass_in | (uintptr_t)mass_out) & 3u) return HS_EINVAL;
+  if (causal && (q_start < 0 || Lq > shape->L || q_start > shape->L - Lq)) return HS_EINVAL;
+  if (!(scale >= 0.f) || !(decay >= 0.f) || !(decay < INFINITY)) return HS_EINVAL;
+  if (tail_k != nullptr) {
+    if (Lq != 1 || causal) return HS_EUNSUPPORTED;
+    if (((uintptr_t)tail_k & 15u) || (tail_lens == nullptr && (tail_len < 0 || tail_len > HS_BT))) return HS_EINVAL;
+  }
+  hs_vec_view q;
+  rc = view_of(Q, shape->B, shape->Hq, Lq, false, &q);
+  if (rc != HS_OK) return rc;
+  hs_mass_args a = {};
+  a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, causal != 0, per_token != 0);
+  if (a.n_ranges > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
+  a.q = q.p; a.q_sb = q.sb; a.q_sh = q.sh; a.q_st = q.st;
+  a.lse = LSE;
+  a.l_sb = lse_strides != nullptr ? lse_strides[0] : (int64_t)shape->Hq * Lq;
+  a.l_sh = lse_strides != nullptr ? lse_strides[1] : Lq;
+  a.tail_k = (const uint16_t*)tail_k; a.tail_lens = tail_lens; a.tail_tiles = tail_tiles; a.tail_len = tail_len; a.tail_tile = tail_tile;
+  a.in = mass_in; a.out = mass_out; a.ws = (float*)workspace;
+  a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.T = shape->L / HS_BT;
+  a.Lq = Lq; a.q_start = q_start; a.causal = causal != 0; a.per_token = per_token != 0;
+  a.scale = scale == 0.f ? 1.0f / sqrtf((float)HS_D) : scale;
+  a.decay = decay;
+  const hipError_t e = hs_launch_mass(a, hs_make_kv_dev(kv), shape->dtype, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* mass, int32_t keep, const int32_t* keeps, int32_t first,
+                   int32_t last, void* workspace, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  rc = check_kv(shape, kv);
+  if (rc != HS_OK) return rc;
+  const int T = shape->L / HS_BT;
+  if (T > kSelectMaxTiles) return HS_EUNSUPPORTED;
+  if (mass == nullptr || ((uintptr_t)mass & 3u) || workspace == nullptr || ((uintptr_t)workspace & 3u) || kv->uniform) return HS_EINVAL;
+  if ((keeps == nullptr && keep < 1) || first < 0 || last < 0) return HS_EINVAL;
+  const hipError_t e = hs_launch_evict(shape->B, shape->Hkv, T, hs_make_kv_dev(kv), mass, keep, keeps, first, last, (int32_t*)workspace,
+                                       (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,
+                   const int64_t weight_strides[2], const int32_t* lens, int32_t keep, int32_t first, int32_t last, void* K_out,
+                   void* V_out, int32_t* index, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  if (n_tokens < 1 || K == nullptr || V == nullptr || weight == nullptr || K_out == nullptr || V_out == nullptr || index == nullptr) return HS_EINVAL;
+  if (n_tokens > 1 << 24) return HS_EUNSUPPORTED;
+  if ((((uintptr_t)K_out | (uintptr_t)V_out) & 15u) || (((uintptr_t)weight | (uintptr_t)index) & 3u)) return HS_EINVAL;
+  if (keep < 1 || first < 0 || last < 0 || (int64_t)first + last > keep) return HS_EINVAL;
+  hs_vec_view k, v;
+  rc = view_of(K, shape->B, shape->Hkv, n_tokens, false, &k);
+  if (rc != HS_OK) return rc;
+  rc = view_of(V, shape->B, shape->Hkv, n_tokens, false, &v);
+  if (rc != HS_OK) return rc;
+  const int64_t w_sb = weight_strides != nullptr ? weight_strides[0] : (int64_t)shape->Hkv * n_tokens;
+  const int64_t w_sh = weight_strides != nullptr ? weight_strides[1] : n_tokens;
+  const hipError_t e = hs_launch_keep(shape->B, shape->Hkv, n_tokens, k, v, weight, w_sb, w_sh, lens, keep, first, last, (uint16_t*)K_out,
+                                      (uint16_t*)V_out, index, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
 }
 
 }  // extern "C"

@@ -214,3 +214,37 @@ hipError_t hs_launch_prefill_narrow_mixed(int teams, int km, int vm, int B, int 
                                           int n_splits, float* ws_o, float* ws_l);
 // most ranges that it chooses from (1: do not split)
 int hs_prefill_auto_splits(int B, int Hq, int Hkv, int T, int Lq, int q_start, int causal, const hs_kv_dev& kv);
+
+// -------- rotary positions, attention mass, eviction, token choice --------
+struct hs_vec_view { uint16_t* p; int64_t sb, sh, st; };  // D-channel vectors: element strides of batch, head, token
+static inline hs_vec_view hs_make_view(const hs_view* v) {
+  if (v == nullptr) return hs_vec_view{nullptr, 0, 0, 0};
+  return hs_vec_view{(uint16_t*)v->data, v->batch, v->head, v->token};
+}
+struct hs_rope_args {
+  hs_rope rope;
+  hs_vec_view q, qo, k, ko, v, vo;
+  const int32_t *positions, *rows;
+  int32_t n, first_position, first_row, n_rows, B, Hq, Hkv;
+};
+hipError_t hs_launch_rope(const hs_rope_args& a, int dtype, hipStream_t st);
+struct hs_mass_args {
+  const uint16_t* q; int64_t q_sb, q_sh, q_st;
+  const float* lse; int64_t l_sb, l_sh;
+  const uint16_t* tail_k;
+  const int32_t *tail_lens, *tail_tiles;
+  const float* in;
+  float* out;
+  float* ws;
+  int32_t B, Hq, Hkv, T, Lq, q_start, causal, tail_len, tail_tile, per_token, n_ranges;
+  float scale, decay;
+};
+// ranges that the queries of a call are cut into; with more than one, ws = n_ranges * B * Hkv * (T or 64 T) floats
+int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_token);
+hipError_t hs_launch_mass(const hs_mass_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);
+// ws: hs_evict_ws_ints ints
+static inline size_t hs_evict_ws_ints(int64_t rows, int T) { return (size_t)rows * (4 + 2 * (size_t)(T + 1)); }
+hipError_t hs_launch_evict(int B, int Hkv, int T, const hs_kv_dev& kv, const float* mass, int keep, const int32_t* keeps, int first, int last,
+                           int32_t* ws, hipStream_t st);
+hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
+                          int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, hipStream_t st);

@@ -1,5 +1,5 @@
-// Argument marshalling of the Python binding in native code: the per-call part of decode, prefill, append, compress and
-// re-compress.  What a call on a small cache costs is mostly this part: in Python with ctypes a decode call of 7 us of
+// Argument marshalling of the Python binding in native code: the per-call part of decode, prefill, append, compress,
+// re-compress and of the calls around a bounded cache.  What a call on a small cache costs is mostly this part: in Python with ctypes a decode call of 7 us of
 // kernels took 13.3 us (8 data_ptr() calls and a ctypes structure for the cache, three allocations, two library calls) and takes
 // 9 here, compressing 2K tokens 16.1 and 8.5.
 //
@@ -16,6 +16,7 @@
 #include <ATen/ops/empty_like.h>
 #include <ATen/record_function.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -39,8 +40,13 @@ struct Entries {  // of libhs.so, as the binding has loaded it
   decltype(&hs_tile_counts) tile_counts;
   decltype(&hs_compress_kv) compress;
   decltype(&hs_recompress_kv) recompress;
+  decltype(&hs_rope_qkv) rope;
+  decltype(&hs_attn_mass) mass;
+  decltype(&hs_attn_mass_workspace_bytes) mass_bytes;
+  decltype(&hs_evict_tiles) evict;
+  decltype(&hs_keep_tokens) keep;
 } g_hs;
-PyTypeObject *g_shape_type, *g_policy_type, *g_kv_type;
+PyTypeObject *g_shape_type, *g_policy_type, *g_kv_type, *g_rope_type;
 
 enum { S_K_DENSE, S_K_NNZ, S_K_META, S_K_MAP, S_V_DENSE, S_V_NNZ, S_V_META, S_V_MAP, S_COUNTS, S_UNIFORM, N_NAMES };
 const char* const kNames[N_NAMES] = {"k_dense", "k_nnz", "k_meta", "k_map", "v_dense", "v_nnz", "v_meta", "v_map", "counts", "uniform"};
@@ -470,11 +476,235 @@ PyObject* recompress(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses in the order of Entries, HsShape, HsPolicy, PackedKV)
+// on the current device, whose current stream the call goes to
+bool here(const at::Tensor& t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
+bool vectors(const at::Tensor& t, at::ScalarType type, int64_t a, int64_t b, int64_t c, int64_t d) {  // [a, b, c, d], channels contiguous
+  return t.scalar_type() == type && t.dim() == 4 && t.size(0) == a && t.size(1) == b && t.size(2) == c && t.size(3) == d && t.stride(3) == 1 && here(t);
+}
+hs_view view(const at::Tensor& t, int head, int token) { return hs_view{t.data_ptr(), t.stride(0), t.stride(head), t.stride(token)}; }
+bool whole(const at::Tensor& t, at::ScalarType type, at::IntArrayRef sizes) {
+  return t.scalar_type() == type && t.sizes() == sizes && t.is_contiguous() && here(t);
+}
+// an int, or an int32 device tensor of these sizes
+bool int_or_rows(PyObject* o, at::IntArrayRef sizes, int32_t* v, const int32_t** rows) {
+  *v = 0;
+  *rows = nullptr;
+  if (!exact_tensor(o)) return get_int(o, v);
+  const at::Tensor& t = tensor(o);
+  if (!whole(t, at::kInt, sizes)) return false;
+  *rows = (const int32_t*)t.data_ptr();
+  return true;
+}
+
+// rope(shape, rope, q, k, v, positions, q_out, k_out, v_out, rows) -> (q_out, k_out, v_out)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  hs_rope r;
+  if (n_args != 10 || !get_shape(a[0], &s) || !get_struct(a[1], g_rope_type, &r, sizeof(r))) Py_RETURN_NONE;
+  for (int i : {2, 3, 4, 6, 7, 8})
+    if (!none_or_tensor(a[i])) Py_RETURN_NONE;
+  const bool has_q = a[2] != Py_None, has_k = a[3] != Py_None, has_v = a[4] != Py_None;
+  if ((!has_q && !has_k) || (has_v && !has_k) || (!has_q && a[6] != Py_None) || (!has_k && a[7] != Py_None) || (!has_v && a[8] != Py_None)) Py_RETURN_NONE;
+  const at::Tensor& some = tensor(has_q ? a[2] : a[3]);
+  if (some.dim() != 4 || some.size(1) > INT32_MAX) Py_RETURN_NONE;
+  const int64_t n = some.size(1);
+  const at::ScalarType type = element_type(s);
+  for (int i = 2; i < 5; i++)
+    if (a[i] != Py_None && !vectors(tensor(a[i]), type, s.B, n, i == 2 ? s.Hq : s.Hkv, s.D)) Py_RETURN_NONE;
+  if (a[6] != Py_None && !vectors(tensor(a[6]), type, s.B, s.Hq, n, s.D)) Py_RETURN_NONE;
+  int64_t n_rows = has_k ? n : 0;
+  for (int i : {8, 7})
+    if (a[i] != Py_None) {
+      if (tensor(a[i]).dim() != 4 || tensor(a[i]).size(2) > INT32_MAX) Py_RETURN_NONE;
+      n_rows = tensor(a[i]).size(2);
+    }
+  for (int i : {7, 8})
+    if (a[i] != Py_None && !vectors(tensor(a[i]), type, s.B, s.Hkv, n_rows, s.D)) Py_RETURN_NONE;
+  int32_t first, row0;
+  const int32_t *positions, *rows;
+  if (!int_or_rows(a[5], {s.B, n}, &first, &positions) || !int_or_rows(a[9], {s.B}, &row0, &rows)) Py_RETURN_NONE;
+  at::Tensor made[3];
+  hs_view in[3], out[3];
+  const bool has[3] = {has_q, has_k, has_v};
+  int rc;
+  {
+    NoGil others_run;
+    for (int i = 0; i < 3; i++) {
+      if (!has[i]) continue;
+      if (a[6 + i] == Py_None) made[i] = NewTensors(some)({s.B, i == 0 ? s.Hq : s.Hkv, i == 0 ? n : n_rows, s.D}, type);
+      in[i] = view(tensor(a[2 + i]), 2, 1);
+      out[i] = view(a[6 + i] == Py_None ? made[i] : tensor(a[6 + i]), 1, 2);
+    }
+    rc = g_hs.rope(&s, &r, (int32_t)n, positions, first, has_q ? &in[0] : nullptr, has_q ? &out[0] : nullptr, has_k ? &in[1] : nullptr,
+                   has_k ? &out[1] : nullptr, has_v ? &in[2] : nullptr, has_v ? &out[2] : nullptr, rows, row0, (int32_t)n_rows, current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  PyObject* result = PyTuple_New(3);
+  for (int i = 0; i < 3 && result != nullptr; i++) {
+    PyObject* o = made[i].defined() ? THPVariable_Wrap(made[i]) : a[6 + i];
+    if (o == nullptr) { Py_DECREF(result); return nullptr; }
+    if (!made[i].defined()) Py_INCREF(o);
+    PyTuple_SET_ITEM(result, i, o);
+  }
+  return result;
+  END_HANDLE_TH_ERRORS
+}
+
+// mass(shape, Q, lse, kv, mass, out, per_token, decay, causal, scale, q_start, tail_k, tail_len, tail_tile, workspace) -> out
+PyObject* mass(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  hs_kv kv;
+  float decay, scale;
+  if (n_args != 15 || !get_shape(a[0], &s) || !exact_tensor(a[1]) || !exact_tensor(a[2]) || !none_or_tensor(a[4]) || !none_or_tensor(a[5]) ||
+      !PyBool_Check(a[6]) || !get_float(a[7], &decay) || !(a[8] == Py_None || PyBool_Check(a[8])) || !get_float(a[9], &scale) ||
+      !none_or_tensor(a[11]) || !none_or_tensor(a[14]) || s.L < 64)
+    Py_RETURN_NONE;
+  const at::Tensor &q = tensor(a[1]), &lse = tensor(a[2]);
+  const bool one = q.dim() == 3;
+  if ((!one && q.dim() != 4) || lse.dim() != q.dim() - 1 || q.scalar_type() != element_type(s) || lse.scalar_type() != at::kFloat || !here(q) || !here(lse))
+    Py_RETURN_NONE;
+  const int64_t Lq = one ? 1 : q.size(2);
+  if (Lq > INT32_MAX || q.size(0) != s.B || q.size(1) != s.Hq || q.size(q.dim() - 1) != s.D || q.stride(q.dim() - 1) != 1 || lse.size(0) != s.B ||
+      lse.size(1) != s.Hq || (!one && (lse.size(2) != Lq || (Lq != 1 && lse.stride(2) != 1))) || !get_kv(a[3], &kv))
+    Py_RETURN_NONE;
+  {
+    PyObject* map = PyObject_GetAttr(a[3], g_names[S_K_MAP]);
+    if (map == nullptr) return nullptr;
+    const bool ok = exact_tensor(map) && here(tensor(map));
+    Py_DECREF(map);
+    if (!ok) Py_RETURN_NONE;
+  }
+  const int per_token = a[6] == Py_True, causal = a[8] == Py_None ? !one : a[8] == Py_True;
+  int32_t q_start = 0;
+  if (causal) {
+    q_start = s.L - (int32_t)Lq;
+    if (a[10] != Py_None && !get_int(a[10], &q_start)) Py_RETURN_NONE;
+  }
+  const int64_t sizes[3] = {s.B, s.Hkv, per_token ? s.L : s.L / 64};
+  for (int i : {4, 5})
+    if (a[i] != Py_None && !whole(tensor(a[i]), at::kFloat, sizes)) Py_RETURN_NONE;
+  int32_t tail_len = 0, tail_tile = 0;
+  const int32_t *lens = nullptr, *tiles = nullptr;
+  if (a[11] != Py_None) {
+    const int64_t tail_sizes[4] = {s.B, s.Hkv, 64, s.D};
+    if (!whole(tensor(a[11]), element_type(s), tail_sizes) || !int_or_rows(a[12], {s.B}, &tail_len, &lens) || !int_or_rows(a[13], {s.B}, &tail_tile, &tiles))
+      Py_RETURN_NONE;
+  }
+  size_t need = 0;
+  if (g_hs.mass_bytes(&s, (int32_t)Lq, causal, per_token, &need) != 0) Py_RETURN_NONE;
+  if (a[14] != Py_None && ((size_t)tensor(a[14]).nbytes() < need || !here(tensor(a[14])))) Py_RETURN_NONE;
+  const bool own_ws = a[14] == Py_None && need != 0, own_out = a[4] == Py_None && a[5] == Py_None;
+  PyObject* to = a[5] != Py_None ? a[5] : a[4];
+  void *ws_ptr = address(a[14]), *out_ptr = address(to);
+  const hs_view qv = one ? hs_view{q.data_ptr(), q.stride(0), q.stride(1), 0} : view(q, 1, 2);
+  const int64_t lse_strides[2] = {lse.stride(0), lse.stride(1)};
+  const float *before = (const float*)address(a[4]), *lse_ptr = (const float*)lse.data_ptr();
+  const void* tk = address(a[11]);
+  at::Tensor out, ws;
+  int rc;
+  {
+    NoGil others_run;
+    if (own_ws || own_out) {
+      const NewTensors make(q);
+      if (own_out) { out = make(sizes, at::kFloat); out_ptr = out.data_ptr(); }
+      if (own_ws) { ws = make.bytes(need); ws_ptr = ws.data_ptr(); }
+    }
+    rc = g_hs.mass(&s, (int32_t)Lq, q_start, scale, causal, &qv, lse_ptr, lse_strides, &kv, tk, tail_len, lens, tail_tile, tiles, per_token, decay,
+                   before, (float*)out_ptr, ws_ptr, current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  if (own_out) return THPVariable_Wrap(out);
+  Py_INCREF(to);
+  return to;
+  END_HANDLE_TH_ERRORS
+}
+
+// evict(shape, cache, mass, keep, first, last, workspace) -> status; the binding marks the cache as not uniform
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  hs_kv kv;
+  int32_t keep, first, last;
+  const int32_t* keeps;
+  if (n_args != 7 || !get_shape(a[0], &s) || !exact_tensor(a[2]) || !get_int(a[4], &first) || !get_int(a[5], &last) || !none_or_tensor(a[6]) || s.L < 64)
+    Py_RETURN_NONE;
+  const int64_t sizes[3] = {s.B, s.Hkv, s.L / 64};
+  const at::Tensor& m = tensor(a[2]);
+  size_t need = 0;
+  if (!whole(m, at::kFloat, sizes) || !int_or_rows(a[3], {s.B, s.Hkv}, &keep, &keeps) || !get_kv(a[1], &kv) || g_hs.workspace_bytes(&s, 4, 0, &need) != 0 ||
+      (a[6] != Py_None && ((size_t)tensor(a[6]).nbytes() < need || !here(tensor(a[6])))))
+    Py_RETURN_NONE;
+  {
+    PyObject* map = PyObject_GetAttr(a[1], g_names[S_K_MAP]);
+    if (map == nullptr) return nullptr;
+    const bool ok = exact_tensor(map) && here(tensor(map));
+    Py_DECREF(map);
+    if (!ok) Py_RETURN_NONE;
+  }
+  kv.uniform = 0;
+  const float* mass_ptr = (const float*)m.data_ptr();
+  void* ws_ptr = address(a[6]);
+  int rc;
+  {
+    NoGil others_run;
+    at::Tensor ws;
+    if (ws_ptr == nullptr) { ws = NewTensors(m).bytes(need); ws_ptr = ws.data_ptr(); }
+    rc = g_hs.evict(&s, &kv, mass_ptr, keep, keeps, first, last, ws_ptr, current_stream());
+  }
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// keep(shape, K, V, weight, keep, first, last, lens) -> (K_out, V_out, index)
+PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  int32_t n_keep, first, last;
+  if (n_args != 8 || !get_shape(a[0], &s) || !exact_tensor(a[1]) || !exact_tensor(a[2]) || !exact_tensor(a[3]) || !get_int(a[4], &n_keep) ||
+      !get_int(a[5], &first) || !get_int(a[6], &last) || !none_or_tensor(a[7]) || n_keep < 1)
+    Py_RETURN_NONE;
+  const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &w = tensor(a[3]);
+  if (k.dim() != 4 || k.size(2) > INT32_MAX) Py_RETURN_NONE;
+  const int64_t n = k.size(2);
+  if (!vectors(k, element_type(s), s.B, s.Hkv, n, s.D) || !vectors(v, element_type(s), s.B, s.Hkv, n, s.D) || w.scalar_type() != at::kFloat ||
+      w.dim() != 3 || w.size(0) != s.B || w.size(1) != s.Hkv || w.size(2) != n || (n != 1 && w.stride(2) != 1) || !here(w) ||
+      (a[7] != Py_None && !whole(tensor(a[7]), at::kInt, {s.B})))
+    Py_RETURN_NONE;
+  const hs_view kv = view(k, 1, 2), vv = view(v, 1, 2);
+  const int64_t strides[2] = {w.stride(0), w.stride(1)};
+  const float* weight = (const float*)w.data_ptr();
+  const int32_t* lens = (const int32_t*)address(a[7]);
+  at::Tensor k_out, v_out, index;
+  int rc;
+  {
+    NoGil others_run;
+    const NewTensors make(k);
+    k_out = make({s.B, s.Hkv, n_keep, s.D}, k.scalar_type());
+    v_out = make({s.B, s.Hkv, n_keep, s.D}, k.scalar_type());
+    index = make({s.B, s.Hkv, n_keep}, at::kInt);
+    rc = g_hs.keep(&s, (int32_t)n, &kv, &vv, weight, strides, lens, n_keep, first, last, k_out.data_ptr(), v_out.data_ptr(), (int32_t*)index.data_ptr(),
+                   current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  const at::Tensor* out[3] = {&k_out, &v_out, &index};
+  PyObject* result = PyTuple_New(3);
+  for (int i = 0; i < 3 && result != nullptr; i++) {
+    PyObject* o = THPVariable_Wrap(*out[i]);
+    if (o == nullptr) { Py_DECREF(result); return nullptr; }
+    PyTuple_SET_ITEM(result, i, o);
+  }
+  return result;
+  END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses in the order of Entries, HsShape, HsPolicy, PackedKV, HsRope)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   constexpr Py_ssize_t n = sizeof(Entries) / sizeof(void*);
-  if (n_args != 4 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != n || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3])) {
-    PyErr_SetString(PyExc_TypeError, "bind(addresses, shape type, policy type, cache type)");
+  if (n_args != 5 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != n || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3]) ||
+      !PyType_Check(a[4])) {
+    PyErr_SetString(PyExc_TypeError, "bind(addresses, shape type, policy type, cache type, rope type)");
     return nullptr;
   }
   void* p[n];
@@ -486,8 +716,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     }
   }
   memcpy(&g_hs, p, sizeof(p));
-  PyTypeObject** types[3] = {&g_shape_type, &g_policy_type, &g_kv_type};
-  for (int i = 0; i < 3; i++) {
+  PyTypeObject** types[4] = {&g_shape_type, &g_policy_type, &g_kv_type, &g_rope_type};
+  for (int i = 0; i < 4; i++) {
     Py_INCREF(a[1 + i]);
     Py_XDECREF(*types[i]);
     *types[i] = (PyTypeObject*)a[1 + i];
@@ -497,6 +727,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 
 #define HS_FN(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {HS_FN(bind), HS_FN(decode), HS_FN(decode_static), HS_FN(prefill), HS_FN(append), HS_FN(pools), HS_FN(compress), HS_FN(recompress),
+                          HS_FN(rope), HS_FN(mass), HS_FN(evict), HS_FN(keep),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_hs_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
