@@ -693,6 +693,10 @@ int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale
   hs_vec_view q;
   rc = view_of(Q, shape->B, shape->Hq, Lq, false, &q);
   if (rc != HS_OK) return rc;
+  // the kernel for many queries reads the queries of 32 / G positions and G heads by 32-bit byte offsets
+  const int64_t l_sh_in = lse_strides != nullptr ? lse_strides[1] : Lq;
+  if (l_sh_in < 0 || (lse_strides != nullptr && lse_strides[0] < 0)) return HS_EINVAL;
+  if ((double)q.st * 62.0 + (double)q.sh * 14.0 >= 4294967040.0 || (double)l_sh_in * 28.0 >= 4294967040.0) return HS_EUNSUPPORTED;
   hs_mass_args a = {};
   a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, causal != 0, per_token != 0);
   if (a.n_ranges > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;

@@ -154,101 +154,168 @@ __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_de
 }
 
 // ---- many queries ----
-// The queries of a kv head's group are numbered query by query, the group's heads side by side (column f: query f / G, head f % G), and pass
-// by in blocks of 32 columns: the B operand of the 32x32x16 matrix instruction, staged in LDS for the workgroup's four waves, which hold
-// a tile of 64 tokens each.  2:4 tiles are expanded once into the dense form: they stay in registers for thousands of queries, the exponentials
-// bound the kernel (16 a lane and 1024 scores; two half-empty sparse products would save matrix time that is not short and cost
-// 16 moves to clear their accumulators), and beside the 32x32 form the vector ALU keeps more of its rate than beside the 16x16 ones.
+// The queries of a kv head's group pass by in blocks of 32 columns (32 / G queries, the group's G heads of each side by side), the B operand of
+// the 32x32 matrix instructions, staged in LDS for the workgroup's four waves, which hold a tile of 64 tokens each.
 //
-// Matrix operands of 32x32x16: lane l = 32 hi + r holds row (column) r and 8 values of k; step (kb, u, half) takes channels
-// 64 kb + 32 u + 16 hi + 8 half + e, in K and Q alike.  Result: column r, rows 8 (i / 4) + 4 hi + i % 4, i = 0..15.
+// Matrix operands: lane l = 32 hi + r holds row (column) r.  Step (kb, u, p) takes 16 channels, 64 kb + 32 u + 16 p + 8 hi + e from lane group hi;
+// a sparse step (kb, u) takes the 32 channels of p = 0 and 1: its B operand is that of the two dense steps, its A operand the
+// kept values of the 16 channels 64 kb + 32 u + 16 hi, a piece of a 2:4 tile as the pool has it.
+// Result: column r, rows 8 (i / 4) + 4 hi + i % 4, i = 0..15.
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 template <bool F16>
 __device__ __forceinline__ f32x16_t mma32(uint4 a, uint4 b, f32x16_t c) {
   if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+template <bool F16, int ABID>
+__device__ __forceinline__ f32x16_t smma32(uint4 a, uint4 b0, uint4 b1, f32x16_t c, int idx) {
+  const hs_u4x2 b{b0, b1};
+  if constexpr (F16) return __builtin_amdgcn_smfmac_f32_32x32x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x16_t, b), c, idx, 0, ABID);
+  else return __builtin_amdgcn_smfmac_f32_32x32x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x16_t, b), c, idx, 0, ABID);
+}
 
-// A tile's operands k[row block][step], from wherever the pool's order has them.
-__device__ __forceinline__ void k_operands(uint4 (&k)[2][8], const hs_kv_dev& kv, int64_t row, int mk, int l) {  // mk != 0, wave-uniform
-  const int hi = l >> 5, r = l & 15, mr = (l >> 4) & 1;
-  if (mk > 0) {
-    const uint8_t* p = kv.k_dense + (row * kv.cap_dense_k + (mk - 1)) * (int64_t)HS_TILE_DENSE_BYTES;
+// Two kept values into their places of four channels.
+__device__ __forceinline__ uint2 spread(uint32_t kept, uint32_t at) {
+  const uint64_t x = ((uint64_t)(kept & 0xffffu) << (16 * (at & 3u))) | ((uint64_t)(kept >> 16) << (16 * ((at >> 2) & 3u)));
+  return make_uint2((uint32_t)x, (uint32_t)(x >> 32));
+}
+
+// A tile's operands, from wherever the pool's order has them, and its products with a block of queries x[step].
+// DENSE: of a tile of either kind, 2:4 ones expanded.
+template <bool F16, bool DENSE>
+struct KTile32 {
+  uint4 k[2][8];  // [row block][step 4 kb + 2 u + p]
+  __device__ __forceinline__ void load(const hs_kv_dev& kv, int64_t row, int mk, int l) {  // mk != 0, wave-uniform
+    const int hi = l >> 5, r = l & 15, mr = (l >> 4) & 1;
+    if (mk > 0) {
+      const uint8_t* p = kv.k_dense + (row * kv.cap_dense_k + (mk - 1)) * (int64_t)HS_TILE_DENSE_BYTES;
+#pragma unroll
+      for (int R = 0; R < 2; R++)
+#pragma unroll
+        for (int s = 0; s < 8; s++) {  // chunk 4 m + 2 kb + u, lane group 2 p + hi
+          const int chunk = 4 * (2 * R + mr) + (s >> 1), lane = 16 * (2 * (s & 1) + hi) + r;
+          k[R][s] = ld_stream(reinterpret_cast<const uint4*>(p + 1024 * chunk + 16 * lane));
+        }
+      return;
+    }
+    const int64_t slot = row * kv.cap_sparse_k + (-mk - 1);
+    const uint8_t* pv = kv.k_nnz + slot * (int64_t)HS_TILE_NNZ_BYTES;
+    const uint8_t* pm = kv.k_meta + slot * (int64_t)HS_TILE_META_BYTES;
+    uint2 kept[2][8];      // channels 8 hi .. 8 hi + 7 of a piece
+    uint32_t idx[2][4];    // [row block][2 u + p]: both kb
 #pragma unroll
     for (int R = 0; R < 2; R++)
 #pragma unroll
-      for (int s = 0; s < 8; s++) {  // s = 4 kb + 2 u + half: chunk 4 m + 2 kb + u, lane group 2 hi + half
-        const int chunk = 4 * (2 * R + mr) + (s >> 1), lane = 16 * (2 * hi + (s & 1)) + r;
-        k[R][s] = ld_stream(reinterpret_cast<const uint4*>(p + 1024 * chunk + 16 * lane));
+      for (int a = 0; a < 4; a++) {
+        const int m = 2 * R + mr, lane = 16 * a + r;
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) kept[R][4 * kb + a] = *reinterpret_cast<const uint2*>(pv + 1024 * (2 * m + kb) + 16 * lane + 8 * hi);
+        idx[R][a] = *reinterpret_cast<const uint32_t*>(pm + 16 * lane + 4 * m);
       }
-    return;
+#pragma unroll
+    for (int R = 0; R < 2; R++)
+#pragma unroll
+      for (int s = 0; s < 8; s++) {
+        const uint32_t at = idx[R][s & 3] >> (16 * (s >> 2) + 8 * hi);
+        const uint2 lo4 = spread(kept[R][s].x, at), hi4 = spread(kept[R][s].y, at >> 4);
+        k[R][s] = make_uint4(lo4.x, lo4.y, hi4.x, hi4.y);
+      }
   }
-  const int64_t slot = row * kv.cap_sparse_k + (-mk - 1);
-  const uint8_t* p = kv.k_nnz + slot * (int64_t)HS_TILE_NNZ_BYTES;
-  const uint8_t* pm = kv.k_meta + slot * (int64_t)HS_TILE_META_BYTES;
-  uint4 kept[2][4];      // [row block][2 kb + u]: 16 channels
+  static constexpr int kSteps = 16;
+  // step i of the products of x into s (both row blocks)
+  __device__ __forceinline__ void step(int i, const uint4 (&x)[8], f32x16_t (&s)[2]) const {
+    const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int st = i >> 1, R = i & 1;
+    s[R] = mma32<F16>(k[R][st], x[st], st == 0 ? zero : s[R]);
+  }
+};
+// 2:4 tiles.  The sparse instruction adds to its accumulators in place: instead of clearing them (32 moves a block) the first 32 channels
+// go through the dense one, expanded.
+template <bool F16>
+struct KTile32<F16, false> {
+  uint4 first[2][2];     // [row block][p]: channels 0 .. 31
+  uint4 k[2][3];         // [row block][sparse step 2 kb + u - 1]
   uint32_t idx[2][2];    // [row block][u]: both kb
+  __device__ __forceinline__ void load(const hs_kv_dev& kv, int64_t row, int mk, int l) {  // mk < 0, wave-uniform
+    const int hi = l >> 5, r = l & 15, mr = (l >> 4) & 1;
+    const int64_t slot = row * kv.cap_sparse_k + (-mk - 1);
+    const uint8_t* pv = kv.k_nnz + slot * (int64_t)HS_TILE_NNZ_BYTES;
+    const uint8_t* pm = kv.k_meta + slot * (int64_t)HS_TILE_META_BYTES;
+    uint2 kept[2][2];
+    uint32_t at[2][2];
 #pragma unroll
-  for (int R = 0; R < 2; R++)
+    for (int R = 0; R < 2; R++) {
+      const int m = 2 * R + mr;
 #pragma unroll
-    for (int u = 0; u < 2; u++) {
-      const int m = 2 * R + mr, lane = 16 * (2 * u + hi) + r;
+      for (int p = 0; p < 2; p++) {
+        const int lane = 16 * p + r;
+        kept[R][p] = *reinterpret_cast<const uint2*>(pv + 1024 * (2 * m) + 16 * lane + 8 * hi);
+        at[R][p] = *reinterpret_cast<const uint32_t*>(pm + 16 * lane + 4 * m);
+      }
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) kept[R][2 * kb + u] = ld_stream(reinterpret_cast<const uint4*>(p + 1024 * (2 * m + kb) + 16 * lane));
-      idx[R][u] = *reinterpret_cast<const uint32_t*>(pm + 16 * lane + 4 * m);
+      for (int s = 1; s < 4; s++) {  // 2 kb + u
+        const int lane = 16 * (2 * (s & 1) + hi) + r;
+        k[R][s - 1] = *reinterpret_cast<const uint4*>(pv + 1024 * (2 * m + (s >> 1)) + 16 * lane);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; u++) idx[R][u] = *reinterpret_cast<const uint32_t*>(pm + 16 * (16 * (2 * u + hi) + r) + 4 * m);
     }
 #pragma unroll
-  for (int R = 0; R < 2; R++)
+    for (int R = 0; R < 2; R++)
 #pragma unroll
-    for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-      for (int u = 0; u < 2; u++) {
-        const uint4 v = kept[R][2 * kb + u];
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w}, where = idx[R][u] >> (16 * kb);
-        uint32_t d[8];
-#pragma unroll
-        for (int q = 0; q < 4; q++) {  // two values into their places of four
-          const uint32_t at = where >> (4 * q);
-          const uint64_t x = ((uint64_t)(w[q] & 0xffffu) << (16 * (at & 3u))) | ((uint64_t)(w[q] >> 16) << (16 * ((at >> 2) & 3u)));
-          d[2 * q] = (uint32_t)x;
-          d[2 * q + 1] = (uint32_t)(x >> 32);
-        }
-        k[R][4 * kb + 2 * u] = make_uint4(d[0], d[1], d[2], d[3]);
-        k[R][4 * kb + 2 * u + 1] = make_uint4(d[4], d[5], d[6], d[7]);
+      for (int p = 0; p < 2; p++) {
+        const uint32_t w = at[R][p] >> (8 * hi);
+        const uint2 lo4 = spread(kept[R][p].x, w), hi4 = spread(kept[R][p].y, w >> 4);
+        first[R][p] = make_uint4(lo4.x, lo4.y, hi4.x, hi4.y);
       }
-}
+  }
+  static constexpr int kSteps = 10;
+  __device__ __forceinline__ void step(int i, const uint4 (&x)[8], f32x16_t (&s)[2]) const {
+    const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int st = i >> 1, R = i & 1;
+    if (st < 2) s[R] = mma32<F16>(first[R][st], x[st], st == 0 ? zero : s[R]);
+    else if (st == 2) s[R] = smma32<F16, 0>(k[R][0], x[2], x[3], s[R], (int)idx[R][1]);
+    else if (st == 3) s[R] = smma32<F16, 1>(k[R][1], x[4], x[5], s[R], (int)idx[R][0]);
+    else s[R] = smma32<F16, 1>(k[R][2], x[6], x[7], s[R], (int)idx[R][1]);
+  }
+};
 
-// Direct loads into LDS, lane l's bytes to base + 16 l (4 l).  Inline assembly: the compiler would wait for all of them in front of any LDS
-// read; they are waited for by count (landed) and a barrier instead.
+// Direct loads into LDS, lane l's bytes to base + 16 l (4 l), from a uniform address + the lane's offset.  Inline assembly: the compiler would
+// wait for all of them in front of any LDS read; they are waited for by count and a barrier instead.
 typedef __attribute__((address_space(3))) void* lptr_t;
-__device__ __forceinline__ void lds_load16(uint32_t base, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"((uint64_t)p) : "memory", "m0");
+__device__ __forceinline__ void lds_load16(uint32_t base, const void* p, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(base), "v"(off), "s"((uint64_t)p) : "memory", "m0");
 }
-__device__ __forceinline__ void lds_load4(uint32_t base, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(base), "v"((uint64_t)p) : "memory", "m0");
+__device__ __forceinline__ void lds_load4(uint32_t base, const void* p, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(base), "v"(off), "s"((uint64_t)p) : "memory", "m0");
 }
 
 constexpr int kStages = 3;                        // a block is requested two blocks ahead
-constexpr int kStageBytes = 8 * 1024 + 4 * 256;   // 8 steps of 64 lanes x 16 bytes, and a copy of the columns' LSE for each wave
+constexpr int kStageBytes = 8 * 1024 + 4 * 256;   // 32 columns of 256 bytes, and a copy of the columns' LSE for each wave
 constexpr int kGroup = 4;                         // tiles of a workgroup
+#ifndef KA
+#define KA 2
+#endif
 
-template <bool F16, bool TOKEN>
+// A block's 32 columns lie in LDS one after the other, the 16-byte chunks of column r exchanged by c -> c ^ (r & 15): loads from memory are of
+// whole 256-byte vectors, 4 to an instruction (as matrix operands, 16 bytes of 64 vectors to an instruction, they cost 500 clocks a
+// block), and reads of one chunk of 32 columns touch every bank alike.
+template <bool F16, bool TOKEN, bool DENSE>
 __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev kv, float scale_log2) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStageBytes];
+  __shared__ __attribute__((aligned(256))) uint8_t lds[kStages * kStageBytes];
   const int tid = threadIdx.x, l = tid & 63, hi = l >> 5, r = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_groups = (A.T + kGroup - 1) / kGroup;
   const int hkv = blockIdx.x % A.Hkv, rest = blockIdx.x / A.Hkv, group = rest % n_groups, range = rest / n_groups, b = blockIdx.y;
-  const int G = A.Hq / A.Hkv;
+  const int G = A.Hq / A.Hkv, Q = 32 / G;  // queries of a block
   const int64_t row = (int64_t)b * A.Hkv + hkv;
   const int t = kGroup * group + w;
   const bool mine = t < A.T;
   const int mk = mine ? __builtin_amdgcn_readfirstlane(kv.k_map[row * A.T + t]) : 0;
   // blocks of this workgroup: its range's, from the first with a query that sees its first tile on
-  const int64_t columns = (int64_t)A.Lq * G;
-  const int blocks = (int)((columns + 31) / 32);
-  const int64_t first_query = A.causal ? max(0, HS_BT * kGroup * group - A.q_start) : 0;
-  const int lo = max((int)((int64_t)blocks * range / A.n_ranges), (int)(first_query * G / 32)), hi_blk = (int)((int64_t)blocks * (range + 1) / A.n_ranges);
+  const int blocks = (A.Lq + Q - 1) / Q;
+  const int lo = max((int)((int64_t)blocks * range / A.n_ranges), A.causal ? max(0, HS_BT * kGroup * group - A.q_start) / Q : 0);
+  const int n = (int)((int64_t)blocks * (range + 1) / A.n_ranges) - lo;
   float acc[2][16];
 #pragma unroll
   for (int R = 0; R < 2; R++)
@@ -256,93 +323,154 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
     for (int i = 0; i < 16; i++) acc[R][i] = 0.f;
   float tile_sum = 0.f;
 
-  if (lo < hi_blk) {
-    uint4 k[2][8];
-    if (mk != 0) k_operands(k, kv, row, mk, l);
+  if (n > 0) {
+    KTile32<F16, DENSE> tile;
+    if (mk != 0) tile.load(kv, row, mk, l);
+    // of these blocks, the first that the wave's tile has any query in, and the first from which on every query sees all of it
+    const int vis = mk == 0 ? n : (A.causal ? max(0, max(0, HS_BT * t - A.q_start) / Q - lo) : 0);
+    const int full = A.causal ? (max(0, HS_BT * t + HS_BT - 1 - A.q_start) + Q - 1) / Q - lo : 0;
+
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lptr_t)lds);
-    // the lane's column of the next block to request
-    const int64_t f0 = (int64_t)32 * lo + r;
-    int qi = (int)(f0 / G), qg = (int)(f0 % G);
-    const int step_i = 32 / G, step_g = 32 % G;
-    const uint16_t* q0 = A.q + b * A.q_sb + (int64_t)hkv * G * A.q_sh + 16 * hi;
-    const float* l0 = A.lse + b * A.l_sb + (int64_t)hkv * G * A.l_sh;
-    auto request = [&](int stage) {
-      const uint32_t at = lds0 + stage * kStageBytes;
-      const int i = min(qi, A.Lq - 1);  // columns past the last read it again and weigh nothing
-      const uint16_t* q = q0 + qg * A.q_sh + i * A.q_st;
-      // steps w and w + 4: (kb, u, half) = (0, w / 2, w % 2) and (1, same)
-      const uint16_t* qw = q + 32 * (w >> 1) + 8 * (w & 1);
-      lds_load16(at + 1024 * w, qw);
-      lds_load16(at + 1024 * (w + 4), qw + 64);
-      lds_load4(at + 8192 + 256 * w, l0 + qg * A.l_sh + i);
-      qi += step_i; qg += step_g;
-      if (qg >= G) { qg -= G; qi++; }
+    // What the lane loads of a block: chunk l % 16 of columns 8 w + l / 16 and the fourth behind it, and the LSE of column r.  Its offset from
+    // the block's first query and head; columns beyond the block's (32 % G) take the first one.
+    auto offset_of = [&](int column) -> uint32_t {
+      const int i = column / G, g = column - i * G;
+      return i < Q ? (uint32_t)(2 * (i * A.q_st + g * A.q_sh)) : 0u;
     };
-    const int n = hi_blk - lo;
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // the tile's own loads: only the requests below are counted from here on
-    request(0);
-    if (n > 1) request(1);
-    int ci = (int)(f0 / G), cg = (int)(f0 % G);  // the lane's column of the block at hand
-    int stage = 0;
-    for (int blk = 0; blk < n; blk++) {
+    const int col0 = 8 * w + (l >> 4), col1 = col0 + 4;
+    const uint32_t chunk0 = 16 * ((l & 15) ^ (col0 & 15)), chunk1 = 16 * ((l & 15) ^ (col1 & 15));
+    const uint32_t off0 = offset_of(col0) + chunk0, off1 = offset_of(col1) + chunk1;
+    const int my_i = r / G, my_g = r - my_i * G;  // the lane's column
+    const uint32_t off_l = my_i < Q ? (uint32_t)(4 * (my_i + my_g * A.l_sh)) : 0u;
+    const uint16_t* q = A.q + b * A.q_sb + (int64_t)hkv * G * A.q_sh + (int64_t)lo * Q * A.q_st;
+    const float* ls = A.lse + b * A.l_sb + (int64_t)hkv * G * A.l_sh + (int64_t)lo * Q;
+    const int64_t q_step = Q * A.q_st;
+    const int n_whole = A.Lq / Q - lo;  // blocks before the one that ends inside
+    auto request = [&](int blk, int stage) {
+      const uint32_t at = lds0 + stage * kStageBytes;
+      uint32_t o0 = off0, o1 = off1, ol = off_l;
+      if (blk >= n_whole) {  // queries past the last: the first of the block again
+        const int there = A.Lq - (lo + blk) * Q;
+        if (col0 / G >= there) o0 = chunk0;
+        if (col1 / G >= there) o1 = chunk1;
+        if (my_i >= there) ol = 0;
+      }
+      lds_load16(at + 2048 * w, q, o0);
+      lds_load16(at + 2048 * w + 1024, q, o1);
+      lds_load4(at + 8192 + 256 * w, ls, ol);
+      q += q_step;
+      ls += Q;
+    };
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // the tile's own loads: only the requests are counted from here on
+    request(0, 0);
+    if (n > 1) request(1, 1);
+
+    int stage = kStages - 1;  // of the block last waited for
+    // Waits for block blk (each one once, in order) and requests the one two further on, into the stage that every wave has left.
+    auto wait_for = [&](int blk) {
       if (blk + 1 < n) asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (blk + 2 < n) request(stage == 0 ? 2 : stage - 1);
-      // visible: the block's last query sees the tile's first token
-      const int64_t f_last = min(columns, (int64_t)32 * (lo + blk + 1)) - 1;
-      const int i_first = __builtin_amdgcn_readfirstlane(ci), i_last = (int)(f_last / G);
-      if (mk != 0 && (!A.causal || A.q_start + i_last >= HS_BT * t)) {
-        const uint4* qs = reinterpret_cast<const uint4*>(lds + stage * kStageBytes);
-        f32x16_t s[2];
+      if (blk + 2 < n) request(blk + 2, stage);
+      stage = stage == kStages - 1 ? 0 : stage + 1;
+    };
+    const uint32_t my_column = 256 * r + 16 * (hi ^ (r & 15)), my_lse = 8192 + 256 * w + 4 * l;
+    auto fetch = [&](uint4 (&x)[8], float& lse) {
+      const uint32_t at = stage * kStageBytes + my_column;
 #pragma unroll
-        for (int R = 0; R < 2; R++)
+      for (int st = 0; st < 8; st++) x[st] = *reinterpret_cast<const uint4*>(lds + (at ^ (32 * st)));  // chunk 2 st + hi
+      lse = *reinterpret_cast<const float*>(lds + stage * kStageBytes + my_lse);
+    };
+    // Columns past the last query and those whose LSE is not finite do not count, nor do tokens that a query does not see.  (Columns beyond the
+    // block's are dropped with their lanes at the end.)
+    auto weigh_seen = [&](const f32x16_t (&s)[2], float lse, int blk) {
+      const int i0 = (lo + blk) * Q + my_i;
+      const bool counts = fabsf(lse) < INFINITY && i0 < A.Lq;
+      const int last = A.causal ? A.q_start + i0 - HS_BT * t : HS_BT;  // last token of the tile that the column sees
+      const float lse2 = lse * kLog2e;
+      float p[32];
 #pragma unroll
-          for (int i = 0; i < 16; i++) s[R][i] = 0.f;
+      for (int e = 0; e < 32; e++) {
+        const bool seen = counts && 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * hi + (e & 3) <= last;
+        p[e] = seen ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -lse2)) : 0.f;
+      }
+      if (TOKEN) {
 #pragma unroll
-        for (int st = 0; st < 8; st++) {
-          const uint4 q = qs[64 * st + l];
+        for (int e = 0; e < 32; e++) acc[e >> 4][e & 15] += p[e];
+      } else {
 #pragma unroll
-          for (int R = 0; R < 2; R++) s[R] = mma32<F16>(k[R][st], q, s[R]);
-        }
-        const float lse = *reinterpret_cast<const float*>(lds + stage * kStageBytes + 8192 + 256 * w + 4 * l);
-        const float lse2 = lse * kLog2e;
-        const bool counts = ci < A.Lq && fabsf(lse) < INFINITY;
-        const bool all_seen = !A.causal || A.q_start + i_first >= HS_BT * t + HS_BT - 1;
-        float p[2][16];
-        if (all_seen && __ballot(!counts) == 0ull) {
+        for (int e = 4; e < 32; e++) p[e & 3] += p[e];
+        tile_sum += (p[0] + p[1]) + (p[2] + p[3]);
+      }
+    };
+    auto all_count = [&](float lse) { return __ballot(!(fabsf(lse) < INFINITY)) == 0ull; };
+    // Where every query sees the whole tile and counts, the products of a block run beside the exponentials of the one before, which a wave
+    // issues without waiting for either: a few scores a lane behind each matrix instruction, the first ones while the queries come
+    // out of LDS.  The order is fixed by hand (left to the scheduler the products came first, one waiting for the other).
+    auto both = [&](f32x16_t (&next)[2], float& lse_next, const f32x16_t (&cur)[2], float lse_cur) {
+      uint4 x[8];
+      fetch(x, lse_next);
+      const float lse2 = lse_cur * kLog2e;
+      float part[4] = {0.f, 0.f, 0.f, 0.f}, p[32];  // tiles: four sums per block first, few roundings
+      auto sum = [&](int e) {
+        if (TOKEN) acc[e >> 4][e & 15] += p[e];
+        else part[e & 3] = e < 4 ? p[e] : part[e & 3] + p[e];
+      };
+      auto two = [&](int g) {  // scores 2 g and 2 g + 1; their sums behind the next pair's exponentials
 #pragma unroll
-          for (int R = 0; R < 2; R++)
+        for (int e = 2 * g; e < 2 * g + 2; e++) p[e] = __builtin_fmaf(cur[e >> 4][e & 15], scale_log2, -lse2);
 #pragma unroll
-            for (int i = 0; i < 16; i++) p[R][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[R][i], scale_log2, -lse2));
-        } else {
-          const int last = A.causal ? A.q_start + ci - HS_BT * t : HS_BT;  // last token of the tile that the column sees
+        for (int e = 2 * g; e < 2 * g + 2; e++) p[e] = __builtin_amdgcn_exp2f(p[e]);
+        if (g > 0) { sum(2 * g - 2); sum(2 * g - 1); }
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      constexpr int kN = KTile32<F16, DENSE>::kSteps;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int R = 0; R < 2; R++)
+      for (int g = 0; g < KA; g++) two(g);
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-              const bool seen = counts && 32 * R + 8 * (i >> 2) + 4 * hi + (i & 3) <= last;
-              p[R][i] = seen ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[R][i], scale_log2, -lse2)) : 0.f;
-            }
-        }
-        if (TOKEN) {
+      for (int i = 0; i < kN; i++) {
+        tile.step(i, x, next);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int R = 0; R < 2; R++)
+        for (int g = KA + (16 - KA) * i / kN; g < KA + (16 - KA) * (i + 1) / kN; g++) two(g);
+      }
+      sum(30); sum(31);
+      if (!TOKEN) tile_sum += (part[0] + part[1]) + (part[2] + part[3]);
+    };
+    f32x16_t s0[2], s1[2];
+    float lse0, lse1;
+    const int n_steady = min(n, n_whole) - 1;  // blocks that have a whole one behind them
+    for (int blk = 0; blk < n;) {
+      wait_for(blk);
+      if (blk < vis) { blk++; continue; }
+      {
+        uint4 x[8];
+        fetch(x, lse0);
 #pragma unroll
-            for (int i = 0; i < 16; i++) acc[R][i] += p[R][i];
-        } else {  // a tree first: few roundings per block
-#pragma unroll
-          for (int d = 8; d >= 1; d >>= 1)
-#pragma unroll
-            for (int i = 0; i < d; i++) {
-              p[0][i] += p[0][i + d];
-              p[1][i] += p[1][i + d];
-            }
-          tile_sum += p[0][0] + p[1][0];
+        for (int i = 0; i < KTile32<F16, DENSE>::kSteps; i++) tile.step(i, x, s0);
+      }
+      if (blk >= full) {
+        for (;;) {
+          if (blk >= n_steady || !all_count(lse0)) break;
+          wait_for(blk + 1);
+          both(s1, lse1, s0, lse0);
+          blk++;
+          if (blk >= n_steady || !all_count(lse1)) {
+            s0[0] = s1[0]; s0[1] = s1[1]; lse0 = lse1;
+            break;
+          }
+          wait_for(blk + 1);
+          both(s0, lse0, s1, lse1);
+          blk++;
         }
       }
-      ci += step_i; cg += step_g;
-      if (cg >= G) { cg -= G; ci++; }
-      stage = stage == kStages - 1 ? 0 : stage + 1;
+      weigh_seen(s0, lse0, blk);
+      blk++;
+    }
+    if (my_i >= Q) {  // no column of any block
+      tile_sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; e++) acc[e >> 4][e & 15] = 0.f;
     }
   }
   if (!mine) return;
@@ -354,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
 #pragma unroll
     for (int i = 0; i < 16; i++) x[i] = (b4 ? acc[1][i] : acc[0][i]) + __shfl_xor(b4 ? acc[0][i] : acc[1][i], 16);
     const float sum = sum_columns(x, l & 15);
-    const int i = l & 15, token = 16 * (l & 16) / 8 + 8 * (i >> 2) + 4 * hi + (i & 3);
+    const int i = l & 15, token = 2 * (l & 16) + 8 * (i >> 2) + 4 * hi + (i & 3);
     const int64_t at = (row * A.T + t) * HS_BT + token;
     if (A.n_ranges == 1) A.out[at] = faded(A, at) + sum;
     else A.ws[range * rows * A.T * HS_BT + at] = sum;
@@ -382,9 +510,9 @@ __global__ __launch_bounds__(256) void mass_join_kernel(hs_mass_args A, int64_t 
 int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_token) {
   (void)causal;
   if (Lq == 1) return 1;
-  const int64_t rows = (int64_t)B * Hkv, groups = rows * ((T + kGroup - 1) / kGroup), blocks = ((int64_t)Lq * (Hq / Hkv) + 31) / 32;
+  const int64_t rows = (int64_t)B * Hkv, groups = rows * ((T + kGroup - 1) / kGroup), queries = 32 / (Hq / Hkv), blocks = (Lq + queries - 1) / queries;
   const int64_t out_bytes = rows * T * (per_token ? HS_BT : 1) * 4;
-  int64_t n = (4096 + groups - 1) / groups;
+  int64_t n = (8192 + groups - 1) / groups;
   if (n > blocks / 16) n = blocks / 16;
   if (n * out_bytes > ((int64_t)64 << 20)) n = ((int64_t)64 << 20) / out_bytes;
   return n < 1 ? 1 : (int)n;
@@ -403,9 +531,11 @@ hipError_t hs_launch_mass(const hs_mass_args& a, const hs_kv_dev& kv, int dtype,
     return hipGetLastError();
   }
   const dim3 grid((unsigned)((a.T + kGroup - 1) / kGroup) * a.n_ranges * a.Hkv, a.B);
-#define HS_MASS(F_, T_) hipLaunchKernelGGL((mass_kernel<F_, T_>), grid, dim3(256), 0, st, a, kv, sl2)
-  if (f16) { if (a.per_token) HS_MASS(true, true); else HS_MASS(true, false); }
-  else { if (a.per_token) HS_MASS(false, true); else HS_MASS(false, false); }
+#define HS_MASS(F_, T_) \
+  if (kv.cap_dense_k == 0) hipLaunchKernelGGL((mass_kernel<F_, T_, false>), grid, dim3(256), 0, st, a, kv, sl2); \
+  else hipLaunchKernelGGL((mass_kernel<F_, T_, true>), grid, dim3(256), 0, st, a, kv, sl2)
+  if (f16) { if (a.per_token) { HS_MASS(true, true); } else { HS_MASS(true, false); } }
+  else { if (a.per_token) { HS_MASS(false, true); } else { HS_MASS(false, false); } }
 #undef HS_MASS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_ranges == 1) return e;
