@@ -12,176 +12,230 @@ namespace {
 // K's in the first half of the list and V's in the second.
 __device__ __forceinline__ int32_t* row_ws(int32_t* ws, int64_t row, int T) { return ws + row * (4 + 2 * (int64_t)(T + 1)); }
 
-// one workgroup per row
 template <int NT>
-__global__ __launch_bounds__(NT) void evict_select_kernel(int T, int4 caps, int32_t* __restrict__ k_map, int32_t* __restrict__ v_map, const float* __restrict__ mass, int keep,
-                                                          const int32_t* __restrict__ keeps, int first, int last, int32_t* __restrict__ ws) {
-  extern __shared__ uint32_t lds[];
-  __shared__ int hist[260], sm[NT / 64], bounds[2], left[4], n_holes[2];
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  k_map += row * T; v_map += row * T; mass += row * T;
-  int32_t* my_ws = row_ws(ws, row, T);
-  const int words = (T + 31) / 32;
-  uint32_t* dropped = lds;                        // a bit per tile
-  uint32_t* marks[2] = {lds + words, lds + 2 * words};         // a bit per slot of the dense and the 2:4 pool
-  uint32_t* before[2] = {lds + 3 * words, lds + 4 * words};    // marks in front of a word
-  if (keeps != nullptr) keep = max(1, keeps[row]);
-
-  // tiles held, and the places between which they may be dropped
-  int n = 0;
-  for (int t0 = 0; t0 < T; t0 += NT) {
-    const int t = t0 + tid;
-    number_of<NT>(t < T && k_map[t] != 0, n, sm);
-  }
-  const int n_drop = min(n - keep, n - min(n, first) - min(n, last));  // may be negative
-  if (n_drop <= 0) {  // the whole workgroup
-    if (tid < 4) my_ws[tid] = 0;
-    return;
-  }
-  if (tid == 0) { bounds[0] = 0; bounds[1] = T; }
-  if (tid < 4) left[tid] = 0;
-  for (int i = tid; i < words; i += NT) dropped[i] = 0;
-  __syncthreads();
-  int seen = 0;
-  for (int t0 = 0; t0 < T; t0 += NT) {
-    const int t = t0 + tid;
-    const bool held = t < T && k_map[t] != 0;
-    const int number = number_of<NT>(held, seen, sm);
-    if (held && number == first) bounds[0] = t;
-    if (held && number == n - last) bounds[1] = t;
-  }
-  __syncthreads();
-  const int lo = bounds[0], hi = bounds[1];
-  auto candidate = [&](int t, uint32_t& key) -> bool {
-    if (k_map[t] == 0) return false;
-    key = rank_key(mass[t]);
-    return true;
-  };
-  const Threshold th = smallest<NT>(lo, hi, n_drop, candidate, hist);
-  int tie = 0;
-  for (int t0 = 0; t0 < T; t0 += NT) {
-    const int t = t0 + tid;
-    const int mk = t < T ? k_map[t] : 0;
-    const bool cand = mk != 0 && t >= lo && t < hi;
-    const uint32_t key = cand ? rank_key(mass[t]) : 0xffffffffu;
-    const int number = number_of<NT>(cand && key == th.key, tie, sm);
-    const bool drop = cand && (key < th.key || (key == th.key && number < th.ties));
-    if (drop) atomicOr(&dropped[t >> 5], 1u << (t & 31));
-    if (mk != 0 && !drop) {
-      atomicAdd(&left[mk > 0 ? 0 : 1], 1);
-      atomicAdd(&left[v_map[t] > 0 ? 2 : 3], 1);
-    }
-  }
-  __syncthreads();
-
-  for (int x = 0; x < 2; x++) {  // K, then V
-    int32_t* map = x == 0 ? k_map : v_map;
-    int32_t* list = my_ws + 4 + x * (T + 1);
-    const int room[2] = {min(T, x == 0 ? caps.x : caps.z), min(T, x == 0 ? caps.y : caps.w)};  // slots of the two pools
-    for (int i = tid; i < 2 * words; i += NT) lds[words + i] = 0;
-    if (tid < 2) n_holes[tid] = 0;
-    __syncthreads();
-    for (int t = tid; t < T; t += NT) {
-      const int m = map[t];
-      if (m == 0) continue;
-      const bool drop = (dropped[t >> 5] >> (t & 31)) & 1u;
-      const int kind = m > 0 ? 0 : 1, slot = (abs(m) & ~HS_MAP_F16) - 1;
-      if (slot < room[kind] && drop == (slot < left[2 * x + kind])) atomicOr(&marks[kind][slot >> 5], 1u << (slot & 31));
-    }
-    __syncthreads();
-    for (int kind = 0; kind < 2; kind++) {  // marks in front of each word
-      int carried = 0;
-      for (int i0 = 0; i0 < words; i0 += NT) {
-        const int i = i0 + tid;
-        int upto = i < words ? __builtin_popcount(marks[kind][i]) : 0;
-        const int mine = upto, l = tid & 63;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int y = __shfl_up(upto, d);
-          if (l >= d) upto += y;
-        }
-        if (l == 63) sm[tid >> 6] = upto;
-        __syncthreads();
-        int off = carried;
-        for (int k = 0; k < NT / 64; k++) {
-          if (k < (tid >> 6)) off += sm[k];
-          carried += sm[k];
-        }
-        if (i < words) {
-          before[kind][i] = off + upto - mine;
-          const int in_front = left[2 * x + kind] - 32 * i;  // slots of the word that are kept for the remaining tiles
-          const uint32_t m = in_front >= 32 ? marks[kind][i] : (in_front <= 0 ? 0u : marks[kind][i] & ((1u << in_front) - 1u));
-          if (m != 0) atomicAdd(&n_holes[kind], __builtin_popcount(m));
-        }
-        __syncthreads();
-      }
-    }
-    // the freed slots, in order
-    for (int kind = 0; kind < 2; kind++)
-      for (int i = tid; i < words; i += NT) {
-        uint32_t m = marks[kind][i];
-        int k = before[kind][i];
-        while (m != 0) {
-          const int slot = 32 * i + __builtin_ctz(m);
-          m &= m - 1;
-          if (slot < left[2 * x + kind]) list[(kind == 0 ? 0 : n_holes[0]) + k] = slot;
-          k++;
-        }
-      }
-    __syncthreads();
-    for (int t = tid; t < T; t += NT) {
-      const int m = map[t];
-      if (m == 0) continue;
-      if ((dropped[t >> 5] >> (t & 31)) & 1u) continue;
-      const int kind = m > 0 ? 0 : 1, slot = (abs(m) & ~HS_MAP_F16) - 1;
-      if (slot >= room[kind] || slot < left[2 * x + kind]) continue;
-      const int k = before[kind][slot >> 5] + __builtin_popcount(marks[kind][slot >> 5] & ((1u << (slot & 31)) - 1u)) - n_holes[kind];
-      if (k < 0 || k >= n_holes[kind]) continue;  // slots that are not 0 .. n - 1: the tile stays
-      const int at = (kind == 0 ? 0 : n_holes[0]) + k, to = list[at];
-      list[at] = (int32_t)((uint32_t)slot << 16 | (uint32_t)to);
-      const int entry = (to + 1) | (abs(m) & HS_MAP_F16);
-      map[t] = m > 0 ? entry : -entry;
-    }
-    __syncthreads();
-    if (tid < 2) my_ws[2 * x + tid] = n_holes[tid];
-    for (int t = tid; t < T; t += NT)
-      if (x == 1 && ((dropped[t >> 5] >> (t & 31)) & 1u)) { k_map[t] = 0; v_map[t] = 0; }
-    __syncthreads();
+__device__ __forceinline__ void copy_slot(const uint8_t* pool, int64_t base, int bytes, uint32_t move) {
+  const uint4* s = reinterpret_cast<const uint4*>(pool + (base + (move >> 16)) * bytes);
+  uint4* d = reinterpret_cast<uint4*>(const_cast<uint8_t*>(pool) + (base + (move & 0xffffu)) * bytes);
+  for (int i = threadIdx.x; i < bytes / 16; i += NT) d[i] = s[i];
+}
+// move i of a row: n0 of dense K, n1 of 2:4 K, n2 of dense V, then of 2:4 V
+template <int NT>
+__device__ __forceinline__ void copy_tile(const hs_kv_dev& kv, int64_t row, int T, const int32_t* my_ws, int i, int n0, int n1, int n2) {
+  const uint32_t move = (uint32_t)my_ws[4 + (i < n0 + n1 ? i : (T + 1) + i - n0 - n1)];
+  if (i < n0) {
+    copy_slot<NT>(kv.k_dense, row * kv.cap_dense_k, HS_TILE_DENSE_BYTES, move);
+  } else if (i < n0 + n1) {
+    copy_slot<NT>(kv.k_nnz, row * kv.cap_sparse_k, HS_TILE_NNZ_BYTES, move);
+    copy_slot<NT>(kv.k_meta, row * kv.cap_sparse_k, HS_TILE_META_BYTES, move);
+  } else if (i < n0 + n1 + n2) {
+    copy_slot<NT>(kv.v_dense, row * kv.cap_dense_v, HS_TILE_DENSE_BYTES, move);
+  } else {
+    copy_slot<NT>(kv.v_nnz, row * kv.cap_sparse_v, HS_TILE_NNZ_BYTES, move);
+    copy_slot<NT>(kv.v_meta, row * kv.cap_sparse_v, HS_TILE_META_BYTES, move);
   }
 }
 
-__device__ __forceinline__ void copy_slot(uint8_t* pool, int64_t base, int bytes, uint32_t move, int tid) {
-  const uint4* s = reinterpret_cast<const uint4*>(pool + (base + (move >> 16)) * bytes);
-  uint4* d = reinterpret_cast<uint4*>(pool + (base + (move & 0xffffu)) * bytes);
-  for (int i = tid; i < bytes / 16; i += 256) d[i] = s[i];
+// One workgroup per row.  A thread holds PER tiles in registers (PER > 0, T <= NT PER), or walks the row's maps (PER == 0).
+// Latency-bound: a chain of a map read, prefix counts, a radix selection and the slots' bookkeeping, about 20 barriers.
+// COPY: the row's moves are made here, too (few, by the host's count); otherwise they are listed for evict_move_kernel.
+template <int NT, int PER, bool COPY>
+__global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const float* __restrict__ mass, int keep, const int32_t* __restrict__ keeps,
+                                                   int first, int last, int32_t* __restrict__ ws) {
+  extern __shared__ uint32_t lds[];
+  constexpr int NW = NT / 64;
+  __shared__ RankScratch rank;
+  __shared__ int counts[NW], left[4], n_holes[4];
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  const int64_t row = blockIdx.x;
+  int32_t* const k_map = const_cast<int32_t*>(kv.k_map) + row * T;
+  int32_t* const v_map = const_cast<int32_t*>(kv.v_map) + row * T;
+  mass += row * T;
+  int32_t* my_ws = row_ws(ws, row, T);
+  const int words = (T + 31) / 32;
+  // dense K, 2:4 K, dense V, 2:4 V
+  uint32_t* const marks = lds;                                             // [4][words]
+  uint16_t* const before = reinterpret_cast<uint16_t*>(lds + 4 * words);   // [4][words]
+  uint32_t* const dropped = lds + 6 * words;                               // [words]
+  const int room[4] = {min(T, kv.cap_dense_k), min(T, kv.cap_sparse_k), min(T, kv.cap_dense_v), min(T, kv.cap_sparse_v)};
+
+  // The row's tiles: PER > 0 in registers, tile j NT + tid in place j.
+  constexpr int kN = PER > 0 ? PER : 1;
+  int mk[kN], mv[kN];
+  uint32_t key[kN];
+  auto tiles = [&](auto fn) {  // fn(tile, k entry, v entry, key) in ascending order of the tile
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int j = 0; j < PER; j++) fn(j * NT + tid, mk[j], mv[j], key[j]);
+    } else {
+      for (int t = tid; t < (T + NT - 1) / NT * NT; t += NT) {
+        const int a = t < T ? k_map[t] : 0;
+        fn(t, a, a != 0 ? v_map[t] : 0, a != 0 ? rank_key(mass[t]) : 0u);
+      }
+    }
+  };
+  if constexpr (PER > 0) {
+    float m[PER];
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+      const int t = j * NT + tid;
+      mk[j] = t < T ? k_map[t] : 0;
+      mv[j] = t < T ? v_map[t] : 0;
+      m[j] = t < T ? mass[t] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; j++) key[j] = rank_key(m[j]);
+  }
+  if (keeps != nullptr) keep = max(1, keeps[row]);
+  for (int i = tid; i < 4 * words; i += NT) marks[i] = 0;
+  for (int i = tid; i < words; i += NT) dropped[i] = 0;
+  if (tid < 4) { left[tid] = 0; n_holes[tid] = 0; }
+
+  // Tiles held, and where the candidates begin and end: behind the first `first` and in front of the last `last` of them.  The held tiles
+  // as bits, whose counts number them.
+  tiles([&](int t, int a, int, uint32_t) {
+    const unsigned long long held = __ballot(a != 0);
+    if (l < 2 && 2 * (t >> 6) + l < words) before[2 * (t >> 6) + l] = (uint16_t)__builtin_popcount((uint32_t)(held >> (32 * l)));  // for now: in the word itself
+  });
+  __syncthreads();
+  // words in chunks of NT: counts in front of each
+  int n = 0;
+  for (int i0 = 0; i0 < words; i0 += NT) {
+    const int i = i0 + tid, mine = i < words ? before[i] : 0;
+    const int upto = wave_upto(mine);
+    if (l == 63) counts[w] = upto;
+    __syncthreads();
+    int off = n;
+#pragma unroll
+    for (int k = 0; k < NW; k++) {
+      if (k < w) off += counts[k];
+      n += counts[k];
+    }
+    if (i < words) before[i] = (uint16_t)(off + upto - mine);  // at most 65535: fewer than T
+    __syncthreads();
+  }
+  const int n_drop = min(n - keep, n - min(n, first) - min(n, last));  // may be negative
+  if (n_drop <= 0) {  // the whole workgroup
+    if (!COPY && tid < 4) my_ws[tid] = 0;
+    return;
+  }
+  // a candidate's number among the held tiles: from `first` on, below n - last
+  auto is_candidate = [&](int t, int a) -> bool {
+    const unsigned long long held = __ballot(a != 0);  // of the wave's 64 tiles, which start at a multiple of 64
+    if (a == 0) return false;
+    const int word = 2 * (t >> 6);
+    const int number = before[word] + __builtin_popcountll(held & ((1ull << l) - 1ull));
+    return number >= first && number < n - last;
+  };
+  uint32_t cands = 0;  // PER > 0: a bit per place
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int j = 0; j < PER; j++) cands |= is_candidate(j * NT + tid, mk[j]) ? 1u << j : 0u;
+  }
+  const uint64_t bound = smallest_bound<NT>(n_drop, [&](auto fn) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int j = 0; j < PER; j++)
+        if ((cands >> j) & 1u) fn(rank_of(key[j], j * NT + tid));
+    } else {
+      tiles([&](int t, int a, int, uint32_t ky) {
+        if (is_candidate(t, a)) fn(rank_of(ky, t));
+      });
+    }
+  }, &rank);
+
+  // what stays of each pool
+  {
+    int stay[4] = {0, 0, 0, 0}, j = 0;
+    tiles([&](int t, int a, int b, uint32_t ky) {
+      const bool cand = PER > 0 ? (cands >> j++) & 1u : is_candidate(t, a);
+      const bool drop = cand && rank_of(ky, t) <= bound;
+      const unsigned long long gone = __ballot(drop);
+      if (l < 2 && 2 * (t >> 6) + l < words) dropped[2 * (t >> 6) + l] = (uint32_t)(gone >> (32 * l));
+      stay[0] += __builtin_popcountll(__ballot(a > 0 && !drop));
+      stay[1] += __builtin_popcountll(__ballot(a < 0 && !drop));
+      stay[2] += __builtin_popcountll(__ballot(b > 0 && !drop));
+      stay[3] += __builtin_popcountll(__ballot(b < 0 && !drop));
+    });
+    if (l < 4) atomicAdd(&left[l], l == 0 ? stay[0] : l == 1 ? stay[1] : l == 2 ? stay[2] : stay[3]);
+  }
+  __syncthreads();
+  auto is_dropped = [&](int t) -> bool { return (dropped[t >> 5] >> (t & 31)) & 1u; };
+  auto mark = [&](int m, int pool, bool drop) {
+    const int slot = (abs(m) & ~HS_MAP_F16) - 1;
+    if (slot < room[pool] && drop == (slot < left[pool])) atomicOr(&marks[pool * words + (slot >> 5)], 1u << (slot & 31));
+  };
+  tiles([&](int t, int a, int b, uint32_t) {
+    if (a == 0) return;
+    const bool drop = is_dropped(t);
+    mark(a, a > 0 ? 0 : 1, drop);
+    mark(b, b > 0 ? 2 : 3, drop);
+  });
+  __syncthreads();
+  // marks in front of each word: a wave a pool
+  if (w < 4) {
+    int carried = 0;
+    for (int i0 = 0; i0 < words; i0 += 64) {
+      const int i = i0 + l;
+      const uint32_t m = i < words ? marks[w * words + i] : 0u;
+      const int upto = wave_upto(__builtin_popcount(m));
+      if (i < words) {
+        before[w * words + i] = (uint16_t)(carried + upto - __builtin_popcount(m));
+        const int in_front = left[w] - 32 * i;  // slots of the word that the remaining tiles take
+        const uint32_t h = in_front >= 32 ? m : (in_front <= 0 ? 0u : m & ((1u << in_front) - 1u));
+        if (h != 0) atomicAdd(&n_holes[w], __builtin_popcount(h));
+      }
+      carried += __shfl(upto, 63);
+    }
+  }
+  __syncthreads();
+  // the freed slots in order, in the list where the moves are going to be: dense, then 2:4
+  auto list_of = [&](int pool) -> int32_t* { return my_ws + 4 + (pool >> 1) * (T + 1) + ((pool & 1) ? n_holes[pool - 1] : 0); };
+  for (int i = tid; i < 4 * words; i += NT) {
+    uint32_t m = marks[i];
+    const int pool = i / words, word = i - pool * words;
+    int k = before[i];
+    while (m != 0) {
+      const int slot = 32 * word + __builtin_ctz(m);
+      m &= m - 1;
+      if (slot < left[pool]) list_of(pool)[k] = slot;
+      k++;
+    }
+  }
+  __syncthreads();
+  auto moved = [&](int m, int pool) -> int {  // the entry of a tile that stays
+    const int slot = (abs(m) & ~HS_MAP_F16) - 1;
+    if (slot >= room[pool] || slot < left[pool]) return m;
+    const int word = pool * words + (slot >> 5);
+    const int k = before[word] + __builtin_popcount(marks[word] & ((1u << (slot & 31)) - 1u)) - n_holes[pool];
+    if (k < 0 || k >= n_holes[pool]) return m;  // slots that are not 0 .. n - 1: the tile stays
+    int32_t* at = list_of(pool) + k;
+    const int to = *at;
+    *at = (int32_t)((uint32_t)slot << 16 | (uint32_t)to);
+    const int entry = (to + 1) | (abs(m) & HS_MAP_F16);
+    return m > 0 ? entry : -entry;
+  };
+  tiles([&](int t, int a, int b, uint32_t) {
+    if (a == 0) return;
+    const bool drop = is_dropped(t);
+    const int na = drop ? 0 : moved(a, a > 0 ? 0 : 1), nb = drop ? 0 : moved(b, b > 0 ? 2 : 3);
+    if (na != a) k_map[t] = na;
+    if (nb != b) v_map[t] = nb;
+  });
+  if (COPY) {
+    __syncthreads();
+    for (int i = 0; i < n_holes[0] + n_holes[1] + n_holes[2] + n_holes[3]; i++)
+      copy_tile<NT>(kv, row, T, my_ws, i, n_holes[0], n_holes[1], n_holes[2]);
+  } else if (tid < 4) {
+    my_ws[tid] = n_holes[tid];
+  }
 }
 
 // grid (any, rows)
 __global__ __launch_bounds__(256) void evict_move_kernel(int T, hs_kv_dev kv, int32_t* __restrict__ ws) {
   const int64_t row = blockIdx.y;
   const int32_t* my_ws = row_ws(ws, row, T);
-  const int n0 = my_ws[0], n1 = my_ws[1], n2 = my_ws[2], n3 = my_ws[3], tid = threadIdx.x;
-  for (int i = blockIdx.x; i < n0 + n1 + n2 + n3; i += gridDim.x) {
-    if (i < n0 + n1) {
-      const uint32_t move = (uint32_t)my_ws[4 + i];
-      if (i < n0) {
-        copy_slot((uint8_t*)kv.k_dense, row * kv.cap_dense_k, HS_TILE_DENSE_BYTES, move, tid);
-      } else {
-        copy_slot((uint8_t*)kv.k_nnz, row * kv.cap_sparse_k, HS_TILE_NNZ_BYTES, move, tid);
-        copy_slot((uint8_t*)kv.k_meta, row * kv.cap_sparse_k, HS_TILE_META_BYTES, move, tid);
-      }
-    } else {
-      const int j = i - n0 - n1;
-      const uint32_t move = (uint32_t)my_ws[4 + (T + 1) + j];
-      if (j < n2) {
-        copy_slot((uint8_t*)kv.v_dense, row * kv.cap_dense_v, HS_TILE_DENSE_BYTES, move, tid);
-      } else {
-        copy_slot((uint8_t*)kv.v_nnz, row * kv.cap_sparse_v, HS_TILE_NNZ_BYTES, move, tid);
-        copy_slot((uint8_t*)kv.v_meta, row * kv.cap_sparse_v, HS_TILE_META_BYTES, move, tid);
-      }
-    }
-  }
+  const int n0 = my_ws[0], n1 = my_ws[1], n2 = my_ws[2], n3 = my_ws[3];
+  for (int i = blockIdx.x; i < n0 + n1 + n2 + n3; i += gridDim.x) copy_tile<256>(kv, row, T, my_ws, i, n0, n1, n2);
 }
 
 }  // namespace
@@ -189,14 +243,23 @@ __global__ __launch_bounds__(256) void evict_move_kernel(int T, hs_kv_dev kv, in
 hipError_t hs_launch_evict(int B, int Hkv, int T, const hs_kv_dev& kv, const float* mass, int keep, const int32_t* keeps, int first, int last,
                            int32_t* ws, hipStream_t st) {
   const int rows = B * Hkv, words = (T + 31) / 32;
-  const size_t lds = 5 * words * sizeof(uint32_t);
-  const int4 caps = make_int4(kv.cap_dense_k, kv.cap_sparse_k, kv.cap_dense_v, kv.cap_sparse_v);
-  if (T <= 1024)
-    hipLaunchKernelGGL((evict_select_kernel<256>), dim3(rows), dim3(256), lds, st, T, caps, (int32_t*)kv.k_map, (int32_t*)kv.v_map, mass, keep, keeps, first, last, ws);
-  else
-    hipLaunchKernelGGL((evict_select_kernel<1024>), dim3(rows), dim3(1024), lds, st, T, caps, (int32_t*)kv.k_map, (int32_t*)kv.v_map, mass, keep, keeps, first, last, ws);
+  const size_t lds = 7 * words * sizeof(uint32_t);
+  // No row can hold more tiles than its pools have slots: with room for few more than `keep` (a cache of fixed size that grows tile by tile) a
+  // row's workgroup makes the few moves itself, and there is one launch.
+  const int most = (int)(min((int64_t)T, min((int64_t)kv.cap_dense_k + kv.cap_sparse_k, (int64_t)kv.cap_dense_v + kv.cap_sparse_v)));
+  const bool copy = keeps == nullptr && most - keep <= 4;
+#define HS_EVICT(NT_, PER_)                                                                                                          \
+  do {                                                                                                                               \
+    if (copy) hipLaunchKernelGGL((evict_kernel<NT_, PER_, true>), dim3(rows), dim3(NT_), lds, st, T, kv, mass, keep, keeps, first, last, ws); \
+    else hipLaunchKernelGGL((evict_kernel<NT_, PER_, false>), dim3(rows), dim3(NT_), lds, st, T, kv, mass, keep, keeps, first, last, ws);     \
+  } while (0)
+  if (T <= 256) HS_EVICT(256, 1);
+  else if (T <= 1024) HS_EVICT(256, 4);
+  else if (T <= 4096) HS_EVICT(1024, 4);
+  else HS_EVICT(1024, 0);
+#undef HS_EVICT
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || copy) return e;
   int per_row = 2048 / rows;
   if (per_row < 1) per_row = 1;
   if (per_row > T) per_row = T;

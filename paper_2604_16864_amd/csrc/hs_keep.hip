@@ -5,11 +5,20 @@
 
 namespace {
 
+// One workgroup per row.  Weights are read three times, the last two from the L2: a histogram of the keys' upper 11 bits finds the bin that the
+// last token kept falls into; that bin's tokens are listed in LDS and ranked there exactly (radix selection over key and place, so that ties go
+// by place); then every wave writes the tokens kept of its own part of the row, behind those of the parts before it.
+constexpr int kBins = 2048, kList = 4096;
 template <int NT>
 __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const float* __restrict__ weight, int64_t w_sb, int64_t w_sh, const int32_t* __restrict__ lens,
                                                          int keep, int first, int last, int32_t* __restrict__ index) {
-  __shared__ int hist[260], sm[NT / 64];
-  const int tid = threadIdx.x;
+  constexpr int NW = NT / 64, U = 8;
+  __shared__ int hist[kBins];
+  __shared__ uint64_t list[kList];
+  __shared__ RankScratch rank;
+  __shared__ int taken[NW], chunk[NT / 64], n_list;
+  __shared__ Bin found;
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
   const int b = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
   weight += b * w_sb + h * w_sh;
   index += (int64_t)blockIdx.x * keep;
@@ -18,20 +27,127 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
     for (int i = tid; i < keep; i += NT) index[i] = i < len ? i : -1;
     return;
   }
-  const int lo = first, hi = len - last, want = keep - first - last;  // first + last <= keep < len
-  Threshold th{0, 0};
-  if (want > 0)  // the largest by the complement of their keys
-    th = smallest<NT>(lo, hi, want, [&](int t, uint32_t& key) -> bool { key = ~rank_key(weight[t]); return true; }, hist);
-  int tie = 0, at = 0;
-  for (int t0 = 0; t0 < len; t0 += NT) {
-    const int t = t0 + tid;
-    const bool cand = want > 0 && t >= lo && t < hi;
-    const uint32_t key = cand ? ~rank_key(weight[t]) : 0xffffffffu;
-    const int number = number_of<NT>(cand && key == th.key, tie, sm);
-    const bool take = t < len && (t < lo || t >= hi || (cand && (key < th.key || (key == th.key && number < th.ties))));
-    const int place = number_of<NT>(take, at, sm);
-    if (take) index[place] = t;
+  const int lo = first, hi = len - last, want = keep - first - last;  // first + last <= keep < len: 0 <= want < hi - lo
+  // the wave's part of the candidates, whole strips of 64
+  const int strips = (hi - lo + 63) / 64, s0 = (int)((int64_t)strips * w / NW), s1 = (int)((int64_t)strips * (w + 1) / NW);
+  // fn(place, key, valid) of U strips at a time; the largest weights have the lowest keys
+  auto part = [&](auto fn) {
+    for (int s = s0; s < s1; s += U) {
+      float x[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int t = lo + 64 * (s + u) + l;
+        x[u] = s + u < s1 && t < hi ? weight[t] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int t = lo + 64 * (s + u) + l;
+        fn(t, ~rank_key(x[u]), s + u < s1 && t < hi);
+      }
+    }
+  };
+  uint64_t bound = 0;  // of the ranks that are taken
+  if (want > 0) {
+    for (int i = tid; i < kBins; i += NT) hist[i] = 0;
+    if (tid < NW) taken[tid] = 0;
+    if (tid == 0) n_list = 0;
+    __syncthreads();
+    part([&](int, uint32_t key, bool valid) {
+      const int bin = (int)(key >> 21);
+      // lanes that share the first one's bin are counted at once: rows of equal weights would take 64 turns at one counter
+      const unsigned long long there = __ballot(valid);
+      if (there == 0ull) return;
+      const int leader = __builtin_ctzll(there);
+      const int its = __builtin_amdgcn_readlane(bin, leader);
+      const unsigned long long alike = __ballot(valid && bin == its);
+      if (l == leader) atomicAdd(&hist[its], __builtin_popcountll(alike));
+      else if (valid && bin != its) atomicAdd(&hist[bin], 1);
+    });
+    __syncthreads();
+    // the bin: sums of NT equal chunks first, then the chunk's bins by wave 0
+    {
+      constexpr int PER = kBins / NT;
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < PER; i++) sum += hist[PER * tid + i];
+      const int upto = wave_upto(sum);
+      if (l == 63) chunk[w] = upto;
+      __syncthreads();
+      int below = upto - sum;
+#pragma unroll
+      for (int k = 0; k < NW; k++)
+        if (k < w) below += chunk[k];
+#pragma unroll
+      for (int i = 0; i < PER; i++) {
+        const int c = hist[PER * tid + i];
+        if (below < want && want <= below + c) found = Bin{PER * tid + i, below, c};
+        below += c;
+      }
+    }
+    __syncthreads();
+    const Bin bin = found;
+    const int rest = want - bin.below;  // of the bin's tokens
+    // the wave's tokens that are taken for certain, and the list of the bin's
+    int sure = 0;
+    const bool whole = rest == bin.in, listed = bin.in <= kList;
+    part([&](int t, uint32_t key, bool valid) {
+      const int its = (int)(key >> 21);
+      sure += __builtin_popcountll(__ballot(valid && (whole ? its <= bin.bin : its < bin.bin)));
+      if (!whole && listed) {
+        const bool mine = valid && its == bin.bin;
+        const unsigned long long all = __ballot(mine);
+        if (all != 0ull) {
+          int at = 0;
+          if (l == 0) at = atomicAdd(&n_list, __builtin_popcountll(all));
+          at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(all & ((1ull << l) - 1ull));
+          if (mine) list[at] = rank_of(key, t);
+        }
+      }
+    });
+    if (l == 0) taken[w] = sure;
+    __syncthreads();
+    if (whole) {
+      bound = (uint64_t)(uint32_t)bin.bin << 53 | (~0ull >> 11);
+    } else if (listed) {
+      bound = smallest_bound<NT>(rest, [&](auto fn) {
+        for (int i = tid; i < bin.in; i += NT) fn(list[i]);
+      }, &rank);
+      for (int i = tid; i < bin.in; i += NT) {
+        const uint64_t r = list[i];
+        if (r <= bound) {  // whose part it is: the last that begins at or before its strip
+          const int strip = ((int)(uint32_t)r - lo) >> 6;
+          int p = (int)(((int64_t)strip * NW) / strips);
+          while (p + 1 < NW && (int)((int64_t)strips * (p + 1) / NW) <= strip) p++;
+          atomicAdd(&taken[p], 1);
+        }
+      }
+    } else {  // most weights alike: ranked where they are
+      bound = smallest_bound<NT>(rest, [&](auto fn) {
+        part([&](int t, uint32_t key, bool valid) {
+          if (valid && (int)(key >> 21) == bin.bin) fn(rank_of(key, t));
+        });
+      }, &rank);
+      int more = 0;
+      part([&](int t, uint32_t key, bool valid) {
+        more += __builtin_popcountll(__ballot(valid && (int)(key >> 21) == bin.bin && rank_of(key, t) <= bound));
+      });
+      if (l == 0) taken[w] += more;
+    }
+    __syncthreads();
   }
+  for (int i = tid; i < first; i += NT) index[i] = i;
+  for (int i = tid; i < last; i += NT) index[keep - last + i] = hi + i;
+  if (want == 0) return;
+  int at = first;
+#pragma unroll
+  for (int k = 0; k < NW; k++)
+    if (k < w) at += taken[k];
+  part([&](int t, uint32_t key, bool valid) {
+    const bool take = valid && rank_of(key, t) <= bound;
+    const unsigned long long all = __ballot(take);
+    if (take) index[at + __builtin_popcountll(all & ((1ull << l) - 1ull))] = t;
+    at += __builtin_popcountll(all);
+  });
 }
 
 // 16 lanes a vector, 16 output rows a workgroup
@@ -56,7 +172,7 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(int Hkv, int keep, hs_
 hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
                           int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, hipStream_t st) {
   const int rows = B * Hkv;
-  if (n <= 1024)
+  if (n <= 4096)
     hipLaunchKernelGGL((keep_select_kernel<256>), dim3(rows), dim3(256), 0, st, Hkv, n, weight, w_sb, w_sh, lens, keep, first, last, index);
   else
     hipLaunchKernelGGL((keep_select_kernel<1024>), dim3(rows), dim3(1024), 0, st, Hkv, n, weight, w_sb, w_sh, lens, keep, first, last, index);

@@ -293,9 +293,7 @@ __device__ __forceinline__ void lds_load4(uint32_t base, const void* p, uint32_t
 constexpr int kStages = 3;                        // a block is requested two blocks ahead
 constexpr int kStageBytes = 8 * 1024 + 4 * 256;   // 32 columns of 256 bytes, and a copy of the columns' LSE for each wave
 constexpr int kGroup = 4;                         // tiles of a workgroup
-#ifndef KA
-#define KA 2
-#endif
+constexpr int kAhead = 2;                         // pairs of exponentials in front of a block's first products
 
 // A block's 32 columns lie in LDS one after the other, the 16-byte chunks of column r exchanged by c -> c ^ (r & 15): loads from memory are of
 // whole 256-byte vectors, 4 to an instruction (as matrix operands, 16 bytes of 64 vectors to an instruction, they cost 500 clocks a
@@ -426,13 +424,13 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
       constexpr int kN = KTile32<F16, DENSE>::kSteps;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int g = 0; g < KA; g++) two(g);
+      for (int g = 0; g < kAhead; g++) two(g);
 #pragma unroll
       for (int i = 0; i < kN; i++) {
         tile.step(i, x, next);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int g = KA + (16 - KA) * i / kN; g < KA + (16 - KA) * (i + 1) / kN; g++) two(g);
+        for (int g = kAhead + (16 - kAhead) * i / kN; g < kAhead + (16 - kAhead) * (i + 1) / kN; g++) two(g);
       }
       sum(30); sum(31);
       if (!TOKEN) tile_sum += (part[0] + part[1]) + (part[2] + part[3]);

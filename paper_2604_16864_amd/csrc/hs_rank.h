@@ -10,67 +10,77 @@ __device__ __forceinline__ uint32_t rank_key(float x) {
   const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
   return b ^ (b & 0x80000000u ? 0xffffffffu : 0x80000000u);
 }
+// What candidates are ranked by: the key, then the place.  No two are equal.
+__device__ __forceinline__ uint64_t rank_of(uint32_t key, int place) { return (uint64_t)key << 32 | (uint32_t)place; }
 
-// Prefix counts over a workgroup of NT threads: each thread's flag is numbered in thread order from `carried` on, which moves on
-// by the count of all.  sm: NT / 64 ints.  Every thread takes part.
-template <int NT>
-__device__ __forceinline__ int number_of(bool flag, int& carried, int* sm) {
-  constexpr int NW = NT / 64;
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const unsigned long long vote = __ballot(flag);
-  if (l == 0) sm[w] = __builtin_popcountll(vote);
-  __syncthreads();
-  int before = carried, all = 0;
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ int wave_upto(int x) {
+  const int l = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < NW; i++) {
-    if (i < w) before += sm[i];
-    all += sm[i];
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (l >= d) x += y;
   }
-  carried += all;
-  __syncthreads();
-  return before + __builtin_popcountll(vote & ((1ull << l) - 1ull));
+  return x;
 }
 
-// The `count` smallest (1 <= count <= how many there are) of the keys that `get` gives for places lo <= t < hi (false: no candidate): those below
-// `key`, and of those equal to it the first `ties` by place.  Radix selection, a byte at a time.
-// hist: 260 ints of LDS.  Every thread takes part.
-struct Threshold { uint32_t key; int ties; };
-template <int NT, typename Get>
-__device__ __forceinline__ Threshold smallest(int lo, int hi, int count, Get get, int* hist) {
-  const int tid = threadIdx.x;
-  uint32_t prefix = 0, mask = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += NT) hist[i] = 0;
-    __syncthreads();
-    for (int t = lo + tid; t < hi; t += NT) {
-      uint32_t key;
-      if (get(t, key) && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1);
-    }
-    __syncthreads();
-    if (tid < 64) {  // lane l: bins 4 l .. 4 l + 3
-      int bin[4], sum = 0;
+// hist[0 .. 64 PER) counted by wave 0: bin and how many are in the bins in front of it, where the sum first reaches `count`.
+struct Bin { int bin, below, in; };
+template <int PER>
+__device__ __forceinline__ void find_bin(const int* hist, int count, Bin* out) {  // wave 0 only
+  const int l = threadIdx.x & 63;
+  int c[PER], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 4; i++) { bin[i] = hist[4 * tid + i]; sum += bin[i]; }
-      int upto = sum;
+  for (int i = 0; i < PER; i++) { c[i] = hist[PER * l + i]; sum += c[i]; }
+  int below = wave_upto(sum) - sum;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(upto, d);
-        if (tid >= d) upto += x;
-      }
-      int below = upto - sum;
+  for (int i = 0; i < PER; i++) {
+    if (below < count && count <= below + c[i]) *out = Bin{PER * l + i, below, c[i]};
+    below += c[i];
+  }
+}
+
+// An upper bound (inclusive) of the `count` smallest ranks, 1 <= count <= how many there are: each(fn) calls fn(rank) for every candidate of
+// this thread.  Radix selection, 8 bits at a time from the first bit in which the candidates differ, until the bin found is taken whole.
+// Every thread takes part; two barriers a pass.
+struct RankScratch { int hist[256]; Bin bin; unsigned long long any[16], all[16]; };
+template <int NT, typename Each>
+__device__ __forceinline__ uint64_t smallest_bound(int count, Each each, RankScratch* s) {
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x, w = tid >> 6;
+  unsigned long long any = 0ull, all = ~0ull;
+  each([&](uint64_t rank) { any |= rank; all &= rank; });
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        if (below < count && count <= below + bin[i]) { hist[256] = 4 * tid + i; hist[257] = count - below; }
-        below += bin[i];
-      }
-    }
+  for (int d = 1; d < 64; d <<= 1) {
+    any |= __shfl_xor(any, d);
+    all &= __shfl_xor(all, d);
+  }
+  if ((tid & 63) == 0) { s->any[w] = any; s->all[w] = all; }
+  for (int i = tid; i < 256; i += NT) s->hist[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; i++) { any |= s->any[i]; all &= s->all[i]; }
+  if (any == all) return any;  // one candidate
+  int top = 64 - __builtin_clzll(any ^ all);  // bits from `top` on are alike
+  uint64_t prefix = top == 64 ? 0ull : any >> top << top;
+  for (;;) {
+    const int low = top > 8 ? top - 8 : 0;
+    const uint64_t same = top == 64 ? 0ull : ~0ull << top;
+    const uint32_t digit = (1u << (top - low)) - 1u;
+    each([&](uint64_t rank) {
+      if ((rank & same) == prefix) atomicAdd(&s->hist[(uint32_t)(rank >> low) & digit], 1);
+    });
     __syncthreads();
-    prefix |= (uint32_t)hist[256] << shift;
-    mask |= 255u << shift;
-    count = hist[257];
+    if (tid < 64) find_bin<4>(s->hist, count, &s->bin);
+    __syncthreads();
+    const Bin b = s->bin;
+    prefix |= (uint64_t)(uint32_t)b.bin << low;
+    count -= b.below;
+    if (b.in == count || low == 0) return prefix | (low == 0 ? 0ull : ~0ull >> (64 - low));
+    top = low;
+    for (int i = tid; i < 256; i += NT) s->hist[i] = 0;
     __syncthreads();
   }
-  return Threshold{prefix, count};
 }
 
 }  // namespace
