@@ -174,7 +174,7 @@ HS_API int hs_tile_counts(const hs_shape* shape, const hs_policy* policy, int32_
 HS_API int hs_kv_bytes(const hs_shape* shape, const int32_t counts[5], size_t bytes[8]);
 
 /* Workspace bytes needed by each call.  [host, pure]
- *   op = 0 compress, 1 prefill (Lq = arg), 2 decode (n_splits = arg, 0 = auto), 3 re-compress, 4 evict
+ *   op = 0 compress, 1 prefill (Lq = arg), 2 decode (n_splits = arg, 0 = auto), 3 re-compress, 4 evict, 5 keep tokens (n_tokens = arg)
  *   (op 1 needs none; op 3 only when the target ranks tiles: then 8 bytes per tile) */
 HS_API int hs_workspace_bytes(const hs_shape* shape, int op, int32_t arg, size_t* bytes);
 
@@ -455,11 +455,12 @@ HS_API int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* m
  *   weight    device fp32, element strides weight_strides[2] = {batch, head} (NULL: contiguous [B, Hkv, n_tokens]), tokens contiguous
  *   index     device int32 [B, Hkv, keep]: the tokens kept
  * A row of fewer than `keep` tokens keeps them all; the rest of its outputs is 0 and its indices -1.  keep >= first + last,
- * keep >= 1, n_tokens <= 2^24.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  No workspace; outputs
- * overlap neither inputs nor each other. */
+ * keep >= 1, n_tokens <= 2^20.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  Outputs overlap neither
+ * inputs nor each other.  workspace: hs_workspace_bytes(op 5, n_tokens), 16-byte aligned (NULL where that is 0), not shared between
+ * two calls in flight; no initial content. */
 HS_API int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,
                    const int64_t weight_strides[2], const int32_t* lens, int32_t keep, int32_t first, int32_t last, void* K_out,
-                   void* V_out, int32_t* index, void* stream);
+                   void* V_out, int32_t* index, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

@@ -114,7 +114,7 @@ EXPORTS = {
     "hs_evict_tiles": (C.c_int, [C.POINTER(HsShape), C.POINTER(HsKV), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
                                  C.c_void_p, C.c_void_p]),
     "hs_keep_tokens": (C.c_int, [C.POINTER(HsShape), C.c_int32, _VIEW, _VIEW, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int32,
-                                 C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+                                 C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "hs_decode_attn_phases": (C.c_int, [C.POINTER(HsShape), C.c_float, C.c_int32, C.c_void_p, C.POINTER(HsKV),
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
 }
@@ -599,7 +599,7 @@ def decode_attn_static(shape, Q, kv, scale=0.0, n_splits=0, out=None, lse=None):
 
 ROPE_HALVES, ROPE_PAIRS = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_STRETCH, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
-OP_EVICT = 4          # hs_workspace_bytes: scratch of evict_tiles
+OP_EVICT, OP_KEEP = 4, 5      # hs_workspace_bytes: scratch of evict_tiles, and of keep_tokens (arg: tokens)
 
 
 def make_rope(rot_dim=HEAD_DIM, layout=ROPE_HALVES, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, low=0.0, high=0.0, trained=0):
@@ -754,9 +754,11 @@ def keep_tokens(shape, K, V, weight, keep, first=0, last=0, lens=None):
         raise HsError("keep_tokens: at least one token is kept")
     K_out = K.new_empty((shape.B, shape.Hkv, keep, shape.D))
     V_out, index = torch.empty_like(K_out), torch.empty(K_out.shape[:3], dtype=torch.int32, device=K.device)
+    need = workspace_bytes(shape, OP_KEEP, n)
+    workspace = _workspace(need, K.device) if need else None
     _check(lib().hs_keep_tokens(C.byref(shape), n, C.byref(_view(K, 1, 2)), C.byref(_view(V, 1, 2)), _ptr(weight),
                                 (C.c_int64 * 2)(weight.stride(0), weight.stride(1)), at, keep, int(first), int(last), _ptr(K_out), _ptr(V_out),
-                                _ptr(index), _stream()))
+                                _ptr(index), _ptr(workspace), _stream()))
     return K_out, V_out, index
 
 

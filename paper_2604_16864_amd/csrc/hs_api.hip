@@ -234,6 +234,10 @@ int hs_workspace_bytes(const hs_shape* shape, int op, int32_t arg, size_t* bytes
     }
     case 3: *bytes = 2 * rows * T * sizeof(int32_t); return HS_OK;
     case 4: *bytes = hs_evict_ws_ints((int64_t)rows, (int)T) * sizeof(int32_t); return HS_OK;
+    case 5:
+      if (arg < 1) return HS_EINVAL;
+      *bytes = hs_keep_ws_bytes((int64_t)rows, arg);
+      return HS_OK;
     default: return HS_EINVAL;
   }
 }
@@ -731,13 +735,14 @@ int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* mass, in
 
 int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,
                    const int64_t weight_strides[2], const int32_t* lens, int32_t keep, int32_t first, int32_t last, void* K_out,
-                   void* V_out, int32_t* index, void* stream) {
+                   void* V_out, int32_t* index, void* workspace, void* stream) {
   int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (n_tokens < 1 || K == nullptr || V == nullptr || weight == nullptr || K_out == nullptr || V_out == nullptr || index == nullptr) return HS_EINVAL;
-  if (n_tokens > 1 << 24) return HS_EUNSUPPORTED;
+  if (n_tokens > 1 << 20) return HS_EUNSUPPORTED;
   if ((((uintptr_t)K_out | (uintptr_t)V_out) & 15u) || (((uintptr_t)weight | (uintptr_t)index) & 3u)) return HS_EINVAL;
   if (keep < 1 || first < 0 || last < 0 || (int64_t)first + last > keep) return HS_EINVAL;
+  if (((uintptr_t)workspace & 15u) || (workspace == nullptr && hs_keep_ws_bytes((int64_t)shape->B * shape->Hkv, n_tokens) != 0)) return HS_EINVAL;
   hs_vec_view k, v;
   rc = view_of(K, shape->B, shape->Hkv, n_tokens, false, &k);
   if (rc != HS_OK) return rc;
@@ -746,7 +751,7 @@ int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, co
   const int64_t w_sb = weight_strides != nullptr ? weight_strides[0] : (int64_t)shape->Hkv * n_tokens;
   const int64_t w_sh = weight_strides != nullptr ? weight_strides[1] : n_tokens;
   const hipError_t e = hs_launch_keep(shape->B, shape->Hkv, n_tokens, k, v, weight, w_sb, w_sh, lens, keep, first, last, (uint16_t*)K_out,
-                                      (uint16_t*)V_out, index, (hipStream_t)stream);
+                                      (uint16_t*)V_out, index, workspace, (hipStream_t)stream);
   return e != hipSuccess ? hip_fail(e) : HS_OK;
 }
 

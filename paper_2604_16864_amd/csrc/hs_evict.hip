@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const fl
 #pragma unroll
     for (int j = 0; j < PER; j++) cands |= is_candidate(j * NT + tid, mk[j]) ? 1u << j : 0u;
   }
-  const uint64_t bound = smallest_bound<NT>(n_drop, [&](auto fn) {
+  auto candidates = [&](auto fn) {
     if constexpr (PER > 0) {
 #pragma unroll
       for (int j = 0; j < PER; j++)
@@ -141,7 +141,9 @@ __global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const fl
         if (is_candidate(t, a)) fn(rank_of(ky, t));
       });
     }
-  }, &rank);
+  };
+  // one tile over, the usual case of a cache that grows by one: no selection
+  const uint64_t bound = n_drop == 1 ? smallest_rank<NT>(candidates, &rank) : smallest_bound<NT>(n_drop, candidates, &rank);
 
   // what stays of each pool
   {

@@ -1,14 +1,29 @@
 // Choice of the tokens that go into a cache: per (batch, kv head) row the first, the last and of the others those of largest weight, in
-// order of position.  One workgroup per row finds them; then their keys and values are gathered.
+// order of position.  Their indices are found by one workgroup per row (short rows) or by three launches of one per part of a row; then their
+// keys and values are gathered.
 #include "hs_common.h"
 #include "hs_rank.h"
 
 namespace {
 
+constexpr int kBins = 2048;
+
+// Counts a wave's keys by their upper bits; lanes that share the first one's bin at once: rows of equal weights would take 64 turns at one counter.
+__device__ __forceinline__ void count_bins(int* hist, uint32_t key, bool valid) {
+  const int bin = (int)(key >> 21), l = threadIdx.x & 63;
+  const unsigned long long there = __ballot(valid);
+  if (there == 0ull) return;
+  const int leader = __builtin_ctzll(there);
+  const int its = __builtin_amdgcn_readlane(bin, leader);
+  const unsigned long long alike = __ballot(valid && bin == its);
+  if (l == leader) atomicAdd(&hist[its], __builtin_popcountll(alike));
+  else if (valid && bin != its) atomicAdd(&hist[bin], 1);
+}
+
 // One workgroup per row.  Weights are read three times, the last two from the L2: a histogram of the keys' upper 11 bits finds the bin that the
 // last token kept falls into; that bin's tokens are listed in LDS and ranked there exactly (radix selection over key and place, so that ties go
 // by place); then every wave writes the tokens kept of its own part of the row, behind those of the parts before it.
-constexpr int kBins = 2048, kList = 4096;
+constexpr int kList = 4096;
 template <int NT>
 __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const float* __restrict__ weight, int64_t w_sb, int64_t w_sh, const int32_t* __restrict__ lens,
                                                          int keep, int first, int last, int32_t* __restrict__ index) {
@@ -52,17 +67,7 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
     if (tid < NW) taken[tid] = 0;
     if (tid == 0) n_list = 0;
     __syncthreads();
-    part([&](int, uint32_t key, bool valid) {
-      const int bin = (int)(key >> 21);
-      // lanes that share the first one's bin are counted at once: rows of equal weights would take 64 turns at one counter
-      const unsigned long long there = __ballot(valid);
-      if (there == 0ull) return;
-      const int leader = __builtin_ctzll(there);
-      const int its = __builtin_amdgcn_readlane(bin, leader);
-      const unsigned long long alike = __ballot(valid && bin == its);
-      if (l == leader) atomicAdd(&hist[its], __builtin_popcountll(alike));
-      else if (valid && bin != its) atomicAdd(&hist[bin], 1);
-    });
+    part([&](int, uint32_t key, bool valid) { count_bins(hist, key, valid); });
     __syncthreads();
     // the bin: sums of NT equal chunks first, then the chunk's bins by wave 0
     {
@@ -150,6 +155,275 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
   });
 }
 
+// ---- long rows ----
+// A workgroup takes a part of a row's candidates, and what one has found the others read in the next launch: (1) a histogram per part of the
+// keys' upper 11 bits; (2) every part adds the row's up, finds the bin that the last token kept falls into, and lists its own
+// tokens of that bin; (3) every part ranks the row's list (the same in each, a few hundred tokens as a rule), and writes the indices of its
+// own tokens kept behind those of the parts before it.  One workgroup a row spends 27 us per 32K tokens on its arithmetic alone.
+constexpr int kParts = 16, kLongList = 8192;
+struct KeepRow {            // per row, in the workspace
+  int32_t bin, rest, in;    // the bin, its tokens that are kept, its tokens
+  int32_t sure[kParts], listed[kParts];  // of a part: tokens kept for certain, tokens of the bin
+  uint32_t any[kParts], all[kParts];     // bits that any / all of a part's keys of the bin have
+};
+struct KeepWs {
+  uint16_t* hist;           // [rows][kParts][kBins]
+  KeepRow* head;            // [rows]
+  uint64_t* list;           // [rows][kLongList]
+};
+__host__ __device__ static inline KeepWs keep_ws(void* ws, int64_t rows) {
+  KeepWs k;
+  k.list = reinterpret_cast<uint64_t*>(ws);
+  k.hist = reinterpret_cast<uint16_t*>(k.list + rows * kLongList);
+  k.head = reinterpret_cast<KeepRow*>(k.hist + rows * kParts * kBins);
+  return k;
+}
+struct KeepArgs {
+  const float* weight;
+  int64_t w_sb, w_sh;
+  const int32_t* lens;
+  int32_t* index;
+  int Hkv, n, keep, first, last;
+};
+// The candidates of a part: strips of 64 tokens, dealt to the waves in contiguous shares.
+struct Part {
+  const float* weight;
+  int len, lo, hi, want, p0, p1, size;  // the part's tokens are p0 .. p1 - 1; size: of a part
+  bool all_kept;
+};
+__device__ __forceinline__ Part part_of(const KeepArgs& A) {
+  const int row = blockIdx.y, b = row / A.Hkv, h = row % A.Hkv;
+  Part p;
+  p.weight = A.weight + b * A.w_sb + h * A.w_sh;
+  p.len = A.lens != nullptr ? min(max(A.lens[b], 0), A.n) : A.n;
+  p.all_kept = p.len <= A.keep;
+  p.lo = A.first; p.hi = p.len - A.last; p.want = A.keep - A.first - A.last;
+  p.size = ((A.n + kParts - 1) / kParts + 255) / 256 * 256;
+  p.p0 = (int)min((int64_t)p.hi, p.lo + (int64_t)p.size * blockIdx.x);
+  p.p1 = (int)min((int64_t)p.hi, (int64_t)p.p0 + p.size);
+  return p;
+}
+// fn(place, key, valid), 8 strips at a time; every lane takes part.  256 threads.
+template <typename Fn>
+__device__ __forceinline__ void of_part(const Part& p, Fn fn) {
+  constexpr int U = 8;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, share = p.size / 4;
+  const int q0 = p.p0 + share * w, q1 = min(p.p1, q0 + share);
+  for (int t0 = q0; t0 < q1; t0 += 64 * U) {
+    float x[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int t = t0 + 64 * u + l;
+      x[u] = t < q1 ? p.weight[t] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int t = t0 + 64 * u + l;
+      fn(t, ~rank_key(x[u]), t < q1);
+    }
+  }
+}
+__global__ __launch_bounds__(256) void keep_count_kernel(KeepArgs A, KeepWs ws) {
+  __shared__ __attribute__((aligned(16))) int hist[kBins];
+  const Part p = part_of(A);
+  if (p.all_kept || p.want == 0) return;
+  for (int i = threadIdx.x; i < kBins; i += 256) hist[i] = 0;
+  __syncthreads();
+  of_part(p, [&](int, uint32_t key, bool valid) { count_bins(hist, key, valid); });
+  __syncthreads();
+  uint32_t* out = reinterpret_cast<uint32_t*>(ws.hist + ((int64_t)blockIdx.y * kParts + blockIdx.x) * kBins);
+  for (int i = threadIdx.x; i < kBins / 2; i += 256) out[i] = (uint32_t)hist[2 * i] | (uint32_t)hist[2 * i + 1] << 16;
+}
+
+__global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
+  __shared__ int chunk[4], sums[4], n_list;
+  __shared__ uint32_t any4[4], all4[4];
+  __shared__ Bin found;
+  const Part p = part_of(A);
+  if (p.all_kept || p.want == 0) return;
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x;
+  const int64_t row = blockIdx.y;
+  // the row's bins 8 tid .. 8 tid + 7, and this part's
+  int sum[8], own[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) sum[i] = own[i] = 0;
+  {
+    const uint4* h = reinterpret_cast<const uint4*>(ws.hist + row * kParts * kBins) + tid;
+    uint4 x[kParts];
+#pragma unroll
+    for (int c = 0; c < kParts; c++) x[c] = h[c * (kBins / 8)];
+#pragma unroll
+    for (int c = 0; c < kParts; c++) {
+      const uint32_t d[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const int v = (int)(i & 1 ? d[i >> 1] >> 16 : d[i >> 1] & 0xffffu);
+        sum[i] += v;
+        if (c == mine) own[i] = v;
+      }
+    }
+  }
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) total += sum[i];
+  const int upto = wave_upto(total);
+  if (l == 63) chunk[w] = upto;
+  if (tid == 0) n_list = 0;
+  __syncthreads();
+  int below = upto - total;
+#pragma unroll
+  for (int k = 0; k < 4; k++)
+    if (k < w) below += chunk[k];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    if (below < p.want && p.want <= below + sum[i]) found = Bin{8 * tid + i, below, sum[i]};
+    below += sum[i];
+  }
+  __syncthreads();
+  const Bin bin = found;
+  int sure = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    if (8 * tid + i < bin.bin) sure += own[i];
+  sure = wave_upto(sure);
+  if (l == 63) sums[w] = sure;
+  // the parts' shares of the list
+  const uint16_t* at_bin = ws.hist + row * kParts * kBins + bin.bin;
+  int before = 0, listed = 0;
+#pragma unroll
+  for (int c = 0; c < kParts; c++) {
+    const int v = at_bin[c * kBins];
+    if (c < mine) before += v;
+    if (c == mine) listed = v;
+  }
+  uint64_t* list = ws.list + row * kLongList + before;
+  const bool write = bin.in <= kLongList;
+  uint32_t any = 0u, all = ~0u;
+  of_part(p, [&](int t, uint32_t key, bool valid) {
+    const bool in = valid && (int)(key >> 21) == bin.bin;
+    const unsigned long long those = __ballot(in);
+    if (those == 0ull) return;
+    if (in) { any |= key; all &= key; }
+    if (!write) return;
+    int at = 0;
+    if (l == 0) at = atomicAdd(&n_list, __builtin_popcountll(those));
+    at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(those & ((1ull << l) - 1ull));
+    if (in) list[at] = rank_of(key, t);
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    any |= __shfl_xor(any, d);
+    all &= __shfl_xor(all, d);
+  }
+  if (l == 0) { any4[w] = any; all4[w] = all; }
+  __syncthreads();
+  if (tid == 0) {
+    KeepRow* r = ws.head + row;
+    if (mine == 0) { r->bin = bin.bin; r->rest = p.want - bin.below; r->in = bin.in; }
+    r->sure[mine] = sums[0] + sums[1] + sums[2] + sums[3];
+    r->listed[mine] = listed;
+    r->any[mine] = any4[0] | any4[1] | any4[2] | any4[3];
+    r->all[mine] = all4[0] & all4[1] & all4[2] & all4[3];
+  }
+}
+
+__global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
+  __shared__ uint64_t list[kLongList];
+  __shared__ RankScratch rank;
+  __shared__ int waves[4], more[4];
+  const Part p = part_of(A);
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x;
+  const int64_t row = blockIdx.y;
+  int32_t* index = A.index + row * A.keep;
+  if (p.all_kept) {
+    for (int i = 256 * mine + tid; i < A.keep; i += 256 * kParts) index[i] = i < p.len ? i : -1;
+    return;
+  }
+  for (int i = 256 * mine + tid; i < A.first; i += 256 * kParts) index[i] = i;
+  for (int i = 256 * mine + tid; i < A.last; i += 256 * kParts) index[A.keep - A.last + i] = p.hi + i;
+  if (p.want == 0) return;
+  const KeepRow* r = ws.head + row;
+  const int bin = r->bin, rest = r->rest, in = r->in;
+  int at = A.first, bins_before = 0, bins_mine = 0;
+  uint32_t any = 0u, all = ~0u;
+#pragma unroll
+  for (int c = 0; c < kParts; c++) {
+    const int s = r->sure[c], b = r->listed[c];
+    if (c < mine) { at += s; bins_before += b; }
+    if (c == mine) bins_mine = b;
+    any |= r->any[c];
+    all &= r->all[c];
+  }
+  // Which tokens of the bin are kept: all; or, their keys alike, the first `rest` by place, of which this part has `mine_of_bin`; or those up
+  // to `bound` in the list.
+  const bool alike = any == all;
+  uint64_t bound = (uint64_t)(uint32_t)bin << 53 | (~0ull >> 11);
+  int mine_of_bin = bins_mine;
+  if (rest < in && alike) {
+    mine_of_bin = min(max(rest - bins_before, 0), bins_mine);
+    at += min(rest, bins_before);
+  } else if (rest == in) {
+    at += bins_before;
+  } else {
+    int kept_before = 0;
+    if (in <= kLongList) {
+      for (int i = tid; i < in; i += 256) list[i] = ws.list[row * kLongList + i];
+      __syncthreads();
+      bound = smallest_bound<256>(rest, [&](auto fn) {
+        for (int i = tid; i < in; i += 256) fn(list[i]);
+      }, &rank);
+      for (int i = tid; i < bins_before; i += 256) kept_before += list[i] <= bound;  // the parts before this one have listed theirs first
+    } else {  // more tokens in one bin than fit the list: every part ranks them where they are
+      auto of_row = [&](int end, auto fn) {
+        for (int t = p.lo + tid; t < end; t += 256) {
+          const uint32_t key = ~rank_key(p.weight[t]);
+          if ((int)(key >> 21) == bin) fn(rank_of(key, t));
+        }
+      };
+      bound = smallest_bound<256>(rest, [&](auto fn) { of_row(p.hi, fn); }, &rank);
+      of_row(p.p0, [&](uint64_t x) { kept_before += x <= bound; });
+    }
+    kept_before = wave_upto(kept_before);
+    if (l == 63) more[w] = kept_before;
+    __syncthreads();
+    at += more[0] + more[1] + more[2] + more[3];
+  }
+  // two passes over the part: how many each wave takes, then their indices
+  auto takes = [&](int t, uint32_t key, bool valid, int& of_bin) -> bool {
+    if (!alike || rest == in) return valid && rank_of(key, t) <= bound;
+    const bool in_bin = valid && (int)(key >> 21) == bin;
+    const unsigned long long those = __ballot(in_bin);
+    const bool take = valid && ((int)(key >> 21) < bin || (in_bin && of_bin + __builtin_popcountll(those & ((1ull << l) - 1ull)) < mine_of_bin));
+    of_bin += __builtin_popcountll(those);
+    return take;
+  };
+  const bool counted = alike && rest < in;
+  int of_bin = 0;
+  if (counted) {  // tokens of the bin in the waves before this one
+    int n = 0;
+    of_part(p, [&](int, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(valid && (int)(key >> 21) == bin)); });
+    if (l == 0) more[w] = n;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+      if (k < w) of_bin += more[k];
+  }
+  int n = 0, ob = of_bin;
+  of_part(p, [&](int t, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(takes(t, key, valid, ob))); });
+  if (l == 0) waves[w] = n;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; k++)
+    if (k < w) at += waves[k];
+  ob = of_bin;
+  of_part(p, [&](int t, uint32_t key, bool valid) {
+    const bool take = takes(t, key, valid, ob);
+    const unsigned long long those = __ballot(take);
+    if (take) index[at + __builtin_popcountll(those & ((1ull << l) - 1ull))] = t;
+    at += __builtin_popcountll(those);
+  });
+}
+
 // 16 lanes a vector, 16 output rows a workgroup
 __global__ __launch_bounds__(256) void keep_gather_kernel(int Hkv, int keep, hs_vec_view K, hs_vec_view V, const int32_t* __restrict__ index, uint16_t* __restrict__ K_out,
                                                           uint16_t* __restrict__ V_out) {
@@ -169,13 +443,26 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(int Hkv, int keep, hs_
 
 }  // namespace
 
+size_t hs_keep_ws_bytes(int64_t rows, int n) {
+  if (n <= HS_KEEP_SHORT) return 0;
+  return (size_t)rows * (kLongList * sizeof(uint64_t) + (size_t)kParts * kBins * sizeof(uint16_t) + sizeof(KeepRow));
+}
+
 hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
-                          int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, hipStream_t st) {
+                          int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, void* ws, hipStream_t st) {
   const int rows = B * Hkv;
-  if (n <= 4096)
+  if (n <= 2048) {
     hipLaunchKernelGGL((keep_select_kernel<256>), dim3(rows), dim3(256), 0, st, Hkv, n, weight, w_sb, w_sh, lens, keep, first, last, index);
-  else
+  } else if (n <= HS_KEEP_SHORT) {
     hipLaunchKernelGGL((keep_select_kernel<1024>), dim3(rows), dim3(1024), 0, st, Hkv, n, weight, w_sb, w_sh, lens, keep, first, last, index);
+  } else {
+    const KeepArgs A{weight, w_sb, w_sh, lens, index, Hkv, n, keep, first, last};
+    const KeepWs k = keep_ws(ws, rows);
+    const dim3 grid(kParts, rows);
+    hipLaunchKernelGGL(keep_count_kernel, grid, dim3(256), 0, st, A, k);
+    hipLaunchKernelGGL(keep_list_kernel, grid, dim3(256), 0, st, A, k);
+    hipLaunchKernelGGL(keep_take_kernel, grid, dim3(256), 0, st, A, k);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(keep_gather_kernel, dim3((keep + 15) / 16, rows), dim3(256), 0, st, Hkv, keep, K, V, index, K_out, V_out);

@@ -44,6 +44,22 @@ __device__ __forceinline__ void find_bin(const int* hist, int count, Bin* out) {
 // this thread.  Radix selection, 8 bits at a time from the first bit in which the candidates differ, until the bin found is taken whole.
 // Every thread takes part; two barriers a pass.
 struct RankScratch { int hist[256]; Bin bin; unsigned long long any[16], all[16]; };
+// The lowest rank of all (~0: no candidate).  One barrier.
+template <int NT, typename Each>
+__device__ __forceinline__ uint64_t smallest_rank(Each each, RankScratch* s) {
+  unsigned long long low = ~0ull;
+  each([&](uint64_t rank) { low = rank < low ? rank : low; });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned long long other = __shfl_xor(low, d);
+    low = other < low ? other : low;
+  }
+  if ((threadIdx.x & 63) == 0) s->any[threadIdx.x >> 6] = low;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NT / 64; i++) low = s->any[i] < low ? s->any[i] : low;
+  return low;
+}
 template <int NT, typename Each>
 __device__ __forceinline__ uint64_t smallest_bound(int count, Each each, RankScratch* s) {
   constexpr int NW = NT / 64;

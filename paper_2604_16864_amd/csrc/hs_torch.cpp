@@ -676,7 +676,9 @@ PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const int64_t strides[2] = {w.stride(0), w.stride(1)};
   const float* weight = (const float*)w.data_ptr();
   const int32_t* lens = (const int32_t*)address(a[7]);
-  at::Tensor k_out, v_out, index;
+  size_t need = 0;
+  if (g_hs.workspace_bytes(&s, 5, (int32_t)n, &need) != 0) Py_RETURN_NONE;
+  at::Tensor k_out, v_out, index, ws;
   int rc;
   {
     NoGil others_run;
@@ -684,8 +686,9 @@ PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     k_out = make({s.B, s.Hkv, n_keep, s.D}, k.scalar_type());
     v_out = make({s.B, s.Hkv, n_keep, s.D}, k.scalar_type());
     index = make({s.B, s.Hkv, n_keep}, at::kInt);
+    if (need != 0) ws = make.bytes(need);
     rc = g_hs.keep(&s, (int32_t)n, &kv, &vv, weight, strides, lens, n_keep, first, last, k_out.data_ptr(), v_out.data_ptr(), (int32_t*)index.data_ptr(),
-                   current_stream());
+                   need != 0 ? ws.data_ptr() : nullptr, current_stream());
   }
   if (rc != 0) return PyLong_FromLong(rc);
   const at::Tensor* out[3] = {&k_out, &v_out, &index};

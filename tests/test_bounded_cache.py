@@ -442,7 +442,7 @@ def _check_evict(sh, kv, maps, mass, keep, first, last, call):
 
 @gpu
 @pytest.mark.parametrize("B,Hkv,T,held,sk,sv", [(1, 1, 1, 1, 1.0, 1.0), (1, 2, 5, 5, 1.0, 0.0), (2, 3, 70, 50, 0.5, 0.5), (2, 2, 300, 300, 0.0, 1.0),
-                                                (1, 2, 256, 200, 0.97, 0.9), (1, 1, 1025, 900, 0.5, 1.0), (2, 1, 1500, 700, 0.2, 0.6)])
+                                                (1, 2, 256, 200, 0.97, 0.9), (1, 1, 1025, 900, 0.5, 1.0), (2, 1, 1500, 700, 0.2, 0.6), (1, 2, 4200, 300, 0.9, 0.8)])
 @pytest.mark.parametrize("shuffle", [False, True])
 def test_evict(B, Hkv, T, held, sk, sv, shuffle):
     for keep, first, last in ((1, 0, 0), (max(1, held - 1), 1, 4), (max(1, held // 4), 1, 4), (max(1, held // 2), 0, 3), (3, 2, 7), (held, 0, 0), (held + 5, 9, 9),
@@ -524,6 +524,24 @@ def test_keep_tokens_ties_zeros_nan_and_infinities():
         _check_keep(sh, K, V, w, keep, 1, 2, None)
     w = torch.full((2, 2, 1500), 0.25, device="cuda")                           # all alike
     _check_keep(sh, K, V, w, 200, 0, 0, [1500, 900])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["spread", "alike", "two values", "mostly zeros", "one bin", "special"])
+def test_keep_tokens_of_rows_in_parts(kind):
+    """Rows long enough to be ranked in parts: weights that differ, that are all or mostly the same, that share their upper bits (more of
+    them than the list of a bin holds, and fewer), and ones that are not numbers."""
+    sh = hb.make_shape(3, 2, 1, TILE)
+    g = _gen(6)
+    for n, keeps in ((4097, (1, 2000, 4096)), (30000, (300, 20000, 29999)), (70000, (50, 69000))):
+        K, V = (torch.randn((3, 1, n, D), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+        x = torch.rand((3, 1, n), generator=g)
+        w = {"spread": torch.exp(4 * torch.randn((3, 1, n), generator=g)), "alike": torch.full((3, 1, n), 0.25), "two values": 1.0 + (x > 0.7).float(),
+             "mostly zeros": torch.where(x > 0.9, x, 0.0), "one bin": 1.0 + x / 8, "special": torch.where(x > 0.5, x, torch.where(x > 0.3, math.nan, torch.where(x > 0.1, -math.inf, -x)))}[kind]
+        for keep in keeps:
+            _check_keep(sh, K, V, w.cuda(), keep, min(keep // 3, 40), min(keep // 3, 70), [n, n // 2 + 7, keep + 1])
+    _check_keep(sh, K, V, w.cuda(), 400, 150, 250, None)                        # none but the ends
+    _check_keep(sh, K, V, w.cuda(), 70000, 1, 2, [70000, 0, 69999])             # all of them
 
 
 @gpu
@@ -786,12 +804,12 @@ def test_refusals_on_the_host():
                     (dict(cache=None), -1), (dict(cache=C.byref(uniform)), -1), (dict(shape=C.byref(hb.make_shape(1, 1, 1, 65537 * 64))), -2)):
         assert evict(**bad) == rc, bad
 
-    def keep(n=100, K=view(), V=view(), w=4096, n_keep=10, first=0, last=0, ko=4096, vo=4096, idx=4096):
-        return L.hs_keep_tokens(s, n, K, V, w, None, None, n_keep, first, last, ko, vo, idx, None)
+    def keep(n=100, K=view(), V=view(), w=4096, n_keep=10, first=0, last=0, ko=4096, vo=4096, idx=4096, ws=4096):
+        return L.hs_keep_tokens(s, n, K, V, w, None, None, n_keep, first, last, ko, vo, idx, ws, None)
 
     for bad, rc in ((dict(n=0), -1), (dict(K=None), -1), (dict(V=None), -1), (dict(w=None), -1), (dict(w=4097), -1), (dict(n_keep=0), -1), (dict(first=-1), -1),
                     (dict(last=-1), -1), (dict(first=6, last=5), -1), (dict(first=2 ** 31 - 1, last=2 ** 31 - 1), -1), (dict(ko=None), -1), (dict(vo=4104), -1),
-                    (dict(idx=None), -1), (dict(n=(1 << 24) + 1), -2), (dict(K=view(token=4)), -1)):
+                    (dict(idx=None), -1), (dict(n=(1 << 20) + 1), -2), (dict(ws=4104), -1), (dict(n=100000, ws=None), -1), (dict(K=view(token=4)), -1)):
         assert keep(**bad) == rc, bad
 
 
