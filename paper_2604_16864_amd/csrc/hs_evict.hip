@@ -186,7 +186,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const fl
         const uint32_t h = in_front >= 32 ? m : (in_front <= 0 ? 0u : m & ((1u << in_front) - 1u));
         if (h != 0) atomicAdd(&n_holes[w], __builtin_popcount(h));
       }
-      carried += __shfl(upto, 63);
+      carried += __builtin_amdgcn_readlane(upto, 63);
     }
   }
   __syncthreads();

@@ -8,16 +8,15 @@ namespace {
 
 constexpr int kBins = 2048;
 
-// Counts a wave's keys by their upper bits; lanes that share the first one's bin at once: rows of equal weights would take 64 turns at one counter.
+// Counts a wave's keys by their upper bits; 64 alike at once: rows of equal weights would take 64 turns at one counter for every 64 tokens.
 __device__ __forceinline__ void count_bins(int* hist, uint32_t key, bool valid) {
-  const int bin = (int)(key >> 21), l = threadIdx.x & 63;
-  const unsigned long long there = __ballot(valid);
-  if (there == 0ull) return;
-  const int leader = __builtin_ctzll(there);
-  const int its = __builtin_amdgcn_readlane(bin, leader);
-  const unsigned long long alike = __ballot(valid && bin == its);
-  if (l == leader) atomicAdd(&hist[its], __builtin_popcountll(alike));
-  else if (valid && bin != its) atomicAdd(&hist[bin], 1);
+  const int bin = (int)(key >> 21);
+  const int one = __builtin_amdgcn_readfirstlane(bin);
+  if (__ballot(valid && bin == one) == ~0ull) {
+    if ((threadIdx.x & 63) == 0) atomicAdd(&hist[one], 64);
+  } else if (valid) {
+    atomicAdd(&hist[bin], 1);
+  }
 }
 
 // One workgroup per row.  Weights are read three times, the last two from the L2: a histogram of the keys' upper 11 bits finds the bin that the
@@ -310,12 +309,8 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
     at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(those & ((1ull << l) - 1ull));
     if (in) list[at] = rank_of(key, t);
   });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    any |= __shfl_xor(any, d);
-    all &= __shfl_xor(all, d);
-  }
-  if (l == 0) { any4[w] = any; all4[w] = all; }
+  const uint64_t bits = wave_or((uint64_t)any << 32 | ~all);
+  if (l == 0) { any4[w] = (uint32_t)(bits >> 32); all4[w] = ~(uint32_t)bits; }
   __syncthreads();
   if (tid == 0) {
     KeepRow* r = ws.head + row;

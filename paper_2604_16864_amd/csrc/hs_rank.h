@@ -6,22 +6,35 @@ namespace {
 
 // Order-preserving bit pattern: a < b as numbers <=> key(a) < key(b); zeros are equal, NaN is below everything.
 __device__ __forceinline__ uint32_t rank_key(float x) {
-  if (x != x) return 0u;
-  const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
-  return b ^ (b & 0x80000000u ? 0xffffffffu : 0x80000000u);
+  const uint32_t b = __float_as_uint(x + 0.f);  // -0 + 0 = 0
+  return x != x ? 0u : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 // What candidates are ranked by: the key, then the place.  No two are equal.
 __device__ __forceinline__ uint64_t rank_of(uint32_t key, int place) { return (uint64_t)key << 32 | (uint32_t)place; }
 
+// Lane movements inside the vector ALU (a lane shuffle goes through the LDS, some 100 clocks each): what a step brings from the lanes below, 0 where
+// there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_below(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+// fn(from_below) for the six steps of an inclusive scan over the wave: lane 63 ends up with all 64
+#define HS_WAVE_STEPS(STEP)                                                                                     \
+  STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
 // Inclusive sums over the lanes of a wave.
 __device__ __forceinline__ int wave_upto(int x) {
-  const int l = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (l >= d) x += y;
-  }
+#define HS_STEP(C_, R_) x += (int)from_below<C_, R_>((uint32_t)x);
+  HS_WAVE_STEPS(HS_STEP)
+#undef HS_STEP
   return x;
+}
+// All lanes' bits or-ed, in every lane.
+__device__ __forceinline__ uint64_t wave_or(uint64_t v) {
+  uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
+#define HS_STEP(C_, R_) lo |= from_below<C_, R_>(lo); hi |= from_below<C_, R_>(hi);
+  HS_WAVE_STEPS(HS_STEP)
+#undef HS_STEP
+  return (uint64_t)__builtin_amdgcn_readlane(hi, 63) << 32 | (uint32_t)__builtin_amdgcn_readlane(lo, 63);
 }
 
 // hist[0 .. 64 PER) counted by wave 0: bin and how many are in the bins in front of it, where the sum first reaches `count`.
@@ -66,11 +79,8 @@ __device__ __forceinline__ uint64_t smallest_bound(int count, Each each, RankScr
   const int tid = threadIdx.x, w = tid >> 6;
   unsigned long long any = 0ull, all = ~0ull;
   each([&](uint64_t rank) { any |= rank; all &= rank; });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    any |= __shfl_xor(any, d);
-    all &= __shfl_xor(all, d);
-  }
+  any = wave_or(any);
+  all = ~wave_or(~all);
   if ((tid & 63) == 0) { s->any[w] = any; s->all[w] = all; }
   for (int i = tid; i < 256; i += NT) s->hist[i] = 0;
   __syncthreads();
