@@ -184,7 +184,6 @@ struct KeepArgs {
   int32_t* index;
   int Hkv, n, keep, first, last;
 };
-// The candidates of a part: strips of 64 tokens, dealt to the waves in contiguous shares.
 struct Part {
   const float* weight;
   int len, lo, hi, want, p0, p1, size;  // the part's tokens are p0 .. p1 - 1; size: of a part
@@ -202,38 +201,59 @@ __device__ __forceinline__ Part part_of(const KeepArgs& A) {
   p.p1 = (int)min((int64_t)p.hi, (int64_t)p.p0 + p.size);
   return p;
 }
-// fn(place, key, valid), 8 strips at a time; every lane takes part.  256 threads.
-template <typename Fn>
-__device__ __forceinline__ void of_part(const Part& p, Fn fn) {
-  constexpr int U = 8;
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, share = p.size / 4;
-  const int q0 = p.p0 + share * w, q1 = min(p.p1, q0 + share);
-  for (int t0 = q0; t0 < q1; t0 += 64 * U) {
-    float x[U];
+// A part's keys, a wave a contiguous share: read once into registers (PER > 0, size <= 256 PER) or 8 strips at a time in every pass (PER == 0).
+// 256 threads.
+template <int PER>
+struct PartKeys {
+  const Part& p;
+  int q0, q1;  // the lane's first token, the end of its wave's
+  uint32_t key[PER > 0 ? PER : 1];
+  __device__ __forceinline__ explicit PartKeys(const Part& part) : p(part) {
+    const int share = p.size / 4;
+    const int start = p.p0 + share * (int)(threadIdx.x >> 6);
+    q0 = start + (int)(threadIdx.x & 63); q1 = min(p.p1, start + share);
+    if constexpr (PER > 0) {
+      float x[PER];
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int t = t0 + 64 * u + l;
-      x[u] = t < q1 ? p.weight[t] : 0.f;
-    }
+      for (int u = 0; u < PER; u++) x[u] = q0 + 64 * u < q1 ? p.weight[q0 + 64 * u] : 0.f;
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int t = t0 + 64 * u + l;
-      fn(t, ~rank_key(x[u]), t < q1);
+      for (int u = 0; u < PER; u++) key[u] = ~rank_key(x[u]);
     }
   }
-}
+  // fn(place, key, valid); every lane takes part
+  template <typename Fn>
+  __device__ __forceinline__ void each(Fn fn) const {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int u = 0; u < PER; u++) fn(q0 + 64 * u, key[u], q0 + 64 * u < q1);
+    } else {
+      constexpr int U = 8;
+      for (int t0 = q0; t0 - (int)(threadIdx.x & 63) < q1; t0 += 64 * U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) x[u] = t0 + 64 * u < q1 ? p.weight[t0 + 64 * u] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; u++) fn(t0 + 64 * u, ~rank_key(x[u]), t0 + 64 * u < q1);
+      }
+    }
+  }
+};
+
+template <int PER>
 __global__ __launch_bounds__(256) void keep_count_kernel(KeepArgs A, KeepWs ws) {
   __shared__ __attribute__((aligned(16))) int hist[kBins];
   const Part p = part_of(A);
   if (p.all_kept || p.want == 0) return;
+  const PartKeys<PER> keys(p);
   for (int i = threadIdx.x; i < kBins; i += 256) hist[i] = 0;
   __syncthreads();
-  of_part(p, [&](int, uint32_t key, bool valid) { count_bins(hist, key, valid); });
+  keys.each([&](int, uint32_t key, bool valid) { count_bins(hist, key, valid); });
   __syncthreads();
   uint32_t* out = reinterpret_cast<uint32_t*>(ws.hist + ((int64_t)blockIdx.y * kParts + blockIdx.x) * kBins);
   for (int i = threadIdx.x; i < kBins / 2; i += 256) out[i] = (uint32_t)hist[2 * i] | (uint32_t)hist[2 * i + 1] << 16;
 }
 
+template <int PER>
 __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
   __shared__ int chunk[4], sums[4], n_list;
   __shared__ uint32_t any4[4], all4[4];
@@ -242,6 +262,7 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
   if (p.all_kept || p.want == 0) return;
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x;
   const int64_t row = blockIdx.y;
+  const PartKeys<PER> keys(p);
   // the row's bins 8 tid .. 8 tid + 7, and this part's
   int sum[8], own[8];
 #pragma unroll
@@ -298,17 +319,24 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
   uint64_t* list = ws.list + row * kLongList + before;
   const bool write = bin.in <= kLongList;
   uint32_t any = 0u, all = ~0u;
-  of_part(p, [&](int t, uint32_t key, bool valid) {
+  int n = 0;  // of the wave's tokens in the bin
+  keys.each([&](int, uint32_t key, bool valid) {
     const bool in = valid && (int)(key >> 21) == bin.bin;
-    const unsigned long long those = __ballot(in);
-    if (those == 0ull) return;
-    if (in) { any |= key; all &= key; }
-    if (!write) return;
-    int at = 0;
-    if (l == 0) at = atomicAdd(&n_list, __builtin_popcountll(those));
-    at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(those & ((1ull << l) - 1ull));
-    if (in) list[at] = rank_of(key, t);
+    n += __builtin_popcountll(__ballot(in));
+    any |= in ? key : 0u;
+    all &= in ? key : ~0u;
   });
+  if (write && n != 0) {
+    int at = 0;
+    if (l == 0) at = atomicAdd(&n_list, n);
+    at = __builtin_amdgcn_readfirstlane(at);
+    keys.each([&](int t, uint32_t key, bool valid) {
+      const bool in = valid && (int)(key >> 21) == bin.bin;
+      const unsigned long long those = __ballot(in);
+      if (in) list[at + __builtin_popcountll(those & ((1ull << l) - 1ull))] = rank_of(key, t);
+      at += __builtin_popcountll(those);
+    });
+  }
   const uint64_t bits = wave_or((uint64_t)any << 32 | ~all);
   if (l == 0) { any4[w] = (uint32_t)(bits >> 32); all4[w] = ~(uint32_t)bits; }
   __syncthreads();
@@ -322,6 +350,7 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
   }
 }
 
+template <int PER>
 __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
   __shared__ uint64_t list[kLongList];
   __shared__ RankScratch rank;
@@ -337,6 +366,7 @@ __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
   for (int i = 256 * mine + tid; i < A.first; i += 256 * kParts) index[i] = i;
   for (int i = 256 * mine + tid; i < A.last; i += 256 * kParts) index[A.keep - A.last + i] = p.hi + i;
   if (p.want == 0) return;
+  const PartKeys<PER> keys(p);
   const KeepRow* r = ws.head + row;
   const int bin = r->bin, rest = r->rest, in = r->in;
   int at = A.first, bins_before = 0, bins_mine = 0;
@@ -396,7 +426,7 @@ __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
   int of_bin = 0;
   if (counted) {  // tokens of the bin in the waves before this one
     int n = 0;
-    of_part(p, [&](int, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(valid && (int)(key >> 21) == bin)); });
+    keys.each([&](int, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(valid && (int)(key >> 21) == bin)); });
     if (l == 0) more[w] = n;
     __syncthreads();
 #pragma unroll
@@ -404,14 +434,14 @@ __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
       if (k < w) of_bin += more[k];
   }
   int n = 0, ob = of_bin;
-  of_part(p, [&](int t, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(takes(t, key, valid, ob))); });
+  keys.each([&](int t, uint32_t key, bool valid) { n += __builtin_popcountll(__ballot(takes(t, key, valid, ob))); });
   if (l == 0) waves[w] = n;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 4; k++)
     if (k < w) at += waves[k];
   ob = of_bin;
-  of_part(p, [&](int t, uint32_t key, bool valid) {
+  keys.each([&](int t, uint32_t key, bool valid) {
     const bool take = takes(t, key, valid, ob);
     const unsigned long long those = __ballot(take);
     if (take) index[at + __builtin_popcountll(those & ((1ull << l) - 1ull))] = t;
@@ -454,9 +484,16 @@ hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, c
     const KeepArgs A{weight, w_sb, w_sh, lens, index, Hkv, n, keep, first, last};
     const KeepWs k = keep_ws(ws, rows);
     const dim3 grid(kParts, rows);
-    hipLaunchKernelGGL(keep_count_kernel, grid, dim3(256), 0, st, A, k);
-    hipLaunchKernelGGL(keep_list_kernel, grid, dim3(256), 0, st, A, k);
-    hipLaunchKernelGGL(keep_take_kernel, grid, dim3(256), 0, st, A, k);
+#define HS_KEEP(PER_)                                                                  \
+  do {                                                                                 \
+    hipLaunchKernelGGL((keep_count_kernel<PER_>), grid, dim3(256), 0, st, A, k);       \
+    hipLaunchKernelGGL((keep_list_kernel<PER_>), grid, dim3(256), 0, st, A, k);        \
+    hipLaunchKernelGGL((keep_take_kernel<PER_>), grid, dim3(256), 0, st, A, k);        \
+  } while (0)
+    if (n <= kParts * 256 * 8) HS_KEEP(8);
+    else if (n <= kParts * 256 * 32) HS_KEEP(32);
+    else HS_KEEP(0);
+#undef HS_KEEP
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -54,8 +54,8 @@ __device__ __forceinline__ void find_bin(const int* hist, int count, Bin* out) {
 }
 
 // An upper bound (inclusive) of the `count` smallest ranks, 1 <= count <= how many there are: each(fn) calls fn(rank) for every candidate of
-// this thread.  Radix selection, 8 bits at a time from the first bit in which the candidates differ, until the bin found is taken whole.
-// Every thread takes part; two barriers a pass.
+// this thread.  Radix selection, 8 bits at a time, passing over bits that no two candidates differ in (weights that came out of a 16-bit
+// format differ in few), until the bin found is taken whole.  Every thread takes part; three barriers a pass.
 struct RankScratch { int hist[256]; Bin bin; unsigned long long any[16], all[16]; };
 // The lowest rank of all (~0: no candidate).  One barrier.
 template <int NT, typename Each>
@@ -87,23 +87,27 @@ __device__ __forceinline__ uint64_t smallest_bound(int count, Each each, RankScr
 #pragma unroll
   for (int i = 0; i < NW; i++) { any |= s->any[i]; all &= s->all[i]; }
   if (any == all) return any;  // one candidate
-  int top = 64 - __builtin_clzll(any ^ all);  // bits from `top` on are alike
-  uint64_t prefix = top == 64 ? 0ull : any >> top << top;
+  const uint64_t differ = any ^ all;
+  uint64_t prefix = all;   // bits found so far, and those that all have
+  uint64_t known = ~differ;
   for (;;) {
-    const int low = top > 8 ? top - 8 : 0;
-    const uint64_t same = top == 64 ? 0ull : ~0ull << top;
+    const uint64_t rest = ~known;  // its highest bit is the digit's highest
+    const int top = 64 - __builtin_clzll(rest), low = top > 8 ? top - 8 : 0;
     const uint32_t digit = (1u << (top - low)) - 1u;
+    const uint64_t above = top == 64 ? 0ull : ~0ull << top;
     each([&](uint64_t rank) {
-      if ((rank & same) == prefix) atomicAdd(&s->hist[(uint32_t)(rank >> low) & digit], 1);
+      if (((rank ^ prefix) & above) == 0ull) atomicAdd(&s->hist[(uint32_t)(rank >> low) & digit], 1);
     });
     __syncthreads();
     if (tid < 64) find_bin<4>(s->hist, count, &s->bin);
     __syncthreads();
     const Bin b = s->bin;
-    prefix |= (uint64_t)(uint32_t)b.bin << low;
+    const uint64_t window = (uint64_t)digit << low;
+    prefix = (prefix & ~window) | (uint64_t)(uint32_t)b.bin << low;
+    known |= window;
     count -= b.below;
-    if (b.in == count || low == 0) return prefix | (low == 0 ? 0ull : ~0ull >> (64 - low));
-    top = low;
+    // taken whole, or the last bits that differ: everything below is in
+    if (b.in == count || known == ~0ull) return known == ~0ull ? prefix : (prefix & above) | (uint64_t)(uint32_t)b.bin << low | ~(above | window);
     for (int i = tid; i < 256; i += NT) s->hist[i] = 0;
     __syncthreads();
   }

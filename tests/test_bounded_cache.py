@@ -533,7 +533,7 @@ def test_keep_tokens_of_rows_in_parts(kind):
     them than the list of a bin holds, and fewer), and ones that are not numbers."""
     sh = hb.make_shape(3, 2, 1, TILE)
     g = _gen(6)
-    for n, keeps in ((4097, (1, 2000, 4096)), (30000, (300, 20000, 29999)), (70000, (50, 69000))):
+    for n, keeps in ((4097, (1, 2000, 4096)), (30000, (300, 20000, 29999)), (32769, (70, 32768)), (70000, (50, 69000)), (140000, (9000,))):
         K, V = (torch.randn((3, 1, n, D), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
         x = torch.rand((3, 1, n), generator=g)
         w = {"spread": torch.exp(4 * torch.randn((3, 1, n), generator=g)), "alike": torch.full((3, 1, n), 0.25), "two values": 1.0 + (x > 0.7).float(),
@@ -541,7 +541,7 @@ def test_keep_tokens_of_rows_in_parts(kind):
         for keep in keeps:
             _check_keep(sh, K, V, w.cuda(), keep, min(keep // 3, 40), min(keep // 3, 70), [n, n // 2 + 7, keep + 1])
     _check_keep(sh, K, V, w.cuda(), 400, 150, 250, None)                        # none but the ends
-    _check_keep(sh, K, V, w.cuda(), 70000, 1, 2, [70000, 0, 69999])             # all of them
+    _check_keep(sh, K, V, w.cuda(), 140000, 1, 2, [140000, 0, 139999])          # all of them
 
 
 @gpu
