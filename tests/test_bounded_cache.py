@@ -93,6 +93,21 @@ def test_rope(B, Hq, Hkv, n, rot, scaling, pairs, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("pairs", [False, True])
+def test_rope_beyond_the_last_level_cache(pairs):
+    """A call of more than 256 MB gives the bits of its parts."""
+    sh = hb.make_shape(2, 32, 8, TILE)
+    rope, _ = _rope(128, pairs, "bands", 500000.0)
+    qkv = torch.randn((2, 8200, 48, D), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    pos = torch.arange(8200, dtype=torch.int32, device="cuda").repeat(2, 1) + 77
+    whole = hb.rope_qkv(sh, rope, qkv[:, :, :32], qkv[:, :, 32:40], qkv[:, :, 40:], positions=pos)
+    for i in range(0, 8200, 1025):
+        x = qkv[:, i:i + 1025]
+        part = hb.rope_qkv(sh, rope, x[:, :, :32], x[:, :, 32:40], x[:, :, 40:], positions=pos[:, i:i + 1025].contiguous())
+        assert all(torch.equal(a[:, :, i:i + 1025], b) for a, b in zip(whole, part)), i
+
+
+@gpu
 @pytest.mark.parametrize("first", [0, 1, -1, 131071, (1 << 31) - 1, -(1 << 31)])
 def test_rope_positions_near_and_far(first):
     """The angle of any int32 position is exact: positions that are a run from `first`, against 64 bits (whose own angle is off by 2^-53 of
