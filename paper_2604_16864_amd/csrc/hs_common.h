@@ -236,7 +236,7 @@ struct hs_mass_args {
   const float* in;
   float* out;
   float* ws;
-  int32_t B, Hq, Hkv, T, Lq, q_start, causal, tail_len, tail_tile, per_token, n_ranges;
+  int32_t B, Hq, Hkv, T, Lq, q_start, causal, tail_len, tail_tile, per_token, n_ranges, numbered;
   float scale, decay;
 };
 // ranges that the queries of a call are cut into; with more than one, ws = n_ranges * B * Hkv * (T or 64 T) floats

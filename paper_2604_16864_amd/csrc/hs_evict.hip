@@ -256,7 +256,7 @@ hipError_t hs_launch_evict(int B, int Hkv, int T, const hs_kv_dev& kv, const flo
     else hipLaunchKernelGGL((evict_kernel<NT_, PER_, false>), dim3(rows), dim3(NT_), lds, st, T, kv, mass, keep, keeps, first, last, ws);     \
   } while (0)
   if (T <= 256) HS_EVICT(256, 1);
-  else if (T <= 1024) HS_EVICT(256, 4);
+  else if (T <= 1024) HS_EVICT(512, 2);
   else if (T <= 4096) HS_EVICT(1024, 4);
   else HS_EVICT(1024, 0);
 #undef HS_EVICT

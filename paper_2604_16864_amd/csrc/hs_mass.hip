@@ -307,12 +307,60 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
   const int hkv = blockIdx.x % A.Hkv, rest = blockIdx.x / A.Hkv, group = rest % n_groups, range = rest / n_groups, b = blockIdx.y;
   const int G = A.Hq / A.Hkv, Q = 32 / G;  // queries of a block
   const int64_t row = (int64_t)b * A.Hkv + hkv;
-  const int t = kGroup * group + w;
-  const bool mine = t < A.T;
-  const int mk = mine ? __builtin_amdgcn_readfirstlane(kv.k_map[row * A.T + t]) : 0;
+  const int64_t rows = (int64_t)A.B * A.Hkv;
+  // The wave's tile: of the row's held ones number kGroup group + w (none: mk == 0, and no query sees it).  Where tiles may be missing the
+  // workgroup numbers them, and its waves write the sums of 0 of the missing ones among the tiles kGroup group + w.
+  int t = kGroup * group + w, t_first = kGroup * group, mk = 0;
+  if (!A.numbered) {
+    if (t < A.T) mk = __builtin_amdgcn_readfirstlane(kv.k_map[row * A.T + t]);
+  } else {
+    __shared__ int counts[8][4], found[kGroup][2];
+    const int32_t* map = kv.k_map + row * A.T;
+    if (t < A.T && map[t] == 0) {  // wave-uniform
+      const int per = TOKEN ? HS_BT : 1;
+      if (l < per) {
+        const int64_t at = (row * A.T + t) * per + l;
+        if (A.n_ranges == 1) A.out[at] = faded(A, at);
+        else A.ws[range * rows * A.T * per + at] = 0.f;
+      }
+    }
+    if (tid < kGroup) found[tid][0] = 0x7fffffff;
+    int carried = 0;
+    for (int base = 0; base < A.T && carried < kGroup * (group + 1); base += 2048) {
+      int m[8];
+#pragma unroll
+      for (int j = 0; j < 8; j++) m[j] = base + 256 * j + tid < A.T ? map[base + 256 * j + tid] : 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        const unsigned long long held = __ballot(m[j] != 0);
+        if (l == 0) counts[j][w] = __builtin_popcountll(held);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        const unsigned long long held = __ballot(m[j] != 0);
+        int before = carried;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          if (k < w) before += counts[j][k];
+          carried += counts[j][k];
+        }
+        const int number = before + __builtin_popcountll(held & ((1ull << l) - 1ull)) - kGroup * group;
+        if (m[j] != 0 && number >= 0 && number < kGroup) { found[number][0] = base + 256 * j + tid; found[number][1] = m[j]; }
+      }
+    }
+    __syncthreads();
+    t_first = __builtin_amdgcn_readfirstlane(found[0][0]);
+    if (t_first == 0x7fffffff) return;  // the whole workgroup: fewer tiles are held
+    t = __builtin_amdgcn_readfirstlane(found[w][0]);
+    mk = t != 0x7fffffff ? __builtin_amdgcn_readfirstlane(found[w][1]) : 0;
+    if (mk == 0) t = A.T;
+  }
+  const bool mine = mk != 0 || (!A.numbered && t < A.T);
   // blocks of this workgroup: its range's, from the first with a query that sees its first tile on
   const int blocks = (A.Lq + Q - 1) / Q;
-  const int lo = max((int)((int64_t)blocks * range / A.n_ranges), A.causal ? max(0, HS_BT * kGroup * group - A.q_start) / Q : 0);
+  const int lo = max((int)((int64_t)blocks * range / A.n_ranges), A.causal ? max(0, HS_BT * t_first - A.q_start) / Q : 0);
   const int n = (int)((int64_t)blocks * (range + 1) / A.n_ranges) - lo;
   float acc[2][16];
 #pragma unroll
@@ -472,8 +520,6 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
     }
   }
   if (!mine) return;
-
-  const int64_t rows = (int64_t)A.B * A.Hkv;
   if (TOKEN) {
     float x[16];
     const bool b4 = l & 16;
@@ -510,8 +556,8 @@ int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_to
   if (Lq == 1) return 1;
   const int64_t rows = (int64_t)B * Hkv, groups = rows * ((T + kGroup - 1) / kGroup), queries = 32 / (Hq / Hkv), blocks = (Lq + queries - 1) / queries;
   const int64_t out_bytes = rows * T * (per_token ? HS_BT : 1) * 4;
-  int64_t n = (8192 + groups - 1) / groups;
-  if (n > blocks / 16) n = blocks / 16;
+  int64_t n = min((8192 + groups - 1) / groups, blocks / 16);
+  n = max(n, min((512 + groups - 1) / groups, blocks / 4));
   if (n * out_bytes > ((int64_t)64 << 20)) n = ((int64_t)64 << 20) / out_bytes;
   return n < 1 ? 1 : (int)n;
 }
@@ -528,10 +574,15 @@ hipError_t hs_launch_mass(const hs_mass_args& a, const hs_kv_dev& kv, int dtype,
 #undef HS_STEP
     return hipGetLastError();
   }
+  // Tiles that may be missing: held ones are numbered (one pass over the row's map per workgroup, 2 us) where workgroups have much to do, or
+  // there are more of them than fit the chip.
+  hs_mass_args m = a;
+  const int64_t workgroups = (int64_t)((a.T + kGroup - 1) / kGroup) * a.n_ranges * a.Hkv * a.B, queries = 32 / (a.Hq / a.Hkv);
+  m.numbered = !kv.uniform && (workgroups > 512 || a.Lq / queries / a.n_ranges >= 16);
   const dim3 grid((unsigned)((a.T + kGroup - 1) / kGroup) * a.n_ranges * a.Hkv, a.B);
 #define HS_MASS(F_, T_) \
-  if (kv.cap_dense_k == 0) hipLaunchKernelGGL((mass_kernel<F_, T_, false>), grid, dim3(256), 0, st, a, kv, sl2); \
-  else hipLaunchKernelGGL((mass_kernel<F_, T_, true>), grid, dim3(256), 0, st, a, kv, sl2)
+  if (kv.cap_dense_k == 0) hipLaunchKernelGGL((mass_kernel<F_, T_, false>), grid, dim3(256), 0, st, m, kv, sl2); \
+  else hipLaunchKernelGGL((mass_kernel<F_, T_, true>), grid, dim3(256), 0, st, m, kv, sl2)
   if (f16) { if (a.per_token) { HS_MASS(true, true); } else { HS_MASS(true, false); } }
   else { if (a.per_token) { HS_MASS(false, true); } else { HS_MASS(false, false); } }
 #undef HS_MASS
