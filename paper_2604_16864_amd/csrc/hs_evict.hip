@@ -192,17 +192,12 @@ __global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const fl
   __syncthreads();
   // the freed slots in order, in the list where the moves are going to be: dense, then 2:4
   auto list_of = [&](int pool) -> int32_t* { return my_ws + 4 + (pool >> 1) * (T + 1) + ((pool & 1) ? n_holes[pool - 1] : 0); };
-  for (int i = tid; i < 4 * words; i += NT) {
-    uint32_t m = marks[i];
-    const int pool = i / words, word = i - pool * words;
-    int k = before[i];
-    while (m != 0) {
-      const int slot = 32 * word + __builtin_ctz(m);
-      m &= m - 1;
-      if (slot < left[pool]) list_of(pool)[k] = slot;
-      k++;
+  for (int pool = 0; pool < 4; pool++)
+    for (int slot = tid; slot < left[pool]; slot += NT) {
+      const int word = pool * words + (slot >> 5);
+      const uint32_t m = marks[word], bit = 1u << (slot & 31);
+      if (m & bit) list_of(pool)[before[word] + __builtin_popcount(m & (bit - 1u))] = slot;
     }
-  }
   __syncthreads();
   auto moved = [&](int m, int pool) -> int {  // the entry of a tile that stays
     const int slot = (abs(m) & ~HS_MAP_F16) - 1;
