@@ -158,23 +158,34 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
 // A workgroup takes a part of a row's candidates, and what one has found the others read in the next launch: (1) a histogram per part of the
 // keys' upper 11 bits; (2) every part adds the row's up, finds the bin that the last token kept falls into, and lists its own
 // tokens of that bin; (3) every part ranks the row's list (the same in each, a few hundred tokens as a rule), and writes the indices of its
-// own tokens kept behind those of the parts before it.  One workgroup a row spends 27 us per 32K tokens on its arithmetic alone.
-constexpr int kParts = 16, kLongList = 8192;
+// own tokens kept behind those of the parts before it.  At most 64 parts: what they have found is a lane each.  One workgroup a row spends 27 us per
+// 32K tokens on its arithmetic alone.
+constexpr int kParts = 64, kLongList = 8192, kLdsList = 2048;
+constexpr int kCoarse = 64, kFine = kBins / kCoarse;  // a histogram's bins, also in sums of 32
 struct KeepRow {            // per row, in the workspace
-  int32_t bin, rest, in;    // the bin, its tokens that are kept, its tokens
+  int32_t bin, rest, in, unused;  // the bin, its tokens that are kept, its tokens
   int32_t sure[kParts], listed[kParts];  // of a part: tokens kept for certain, tokens of the bin
   uint32_t any[kParts], all[kParts];     // bits that any / all of a part's keys of the bin have
 };
 struct KeepWs {
-  uint16_t* hist;           // [rows][kParts][kBins]
-  KeepRow* head;            // [rows]
   uint64_t* list;           // [rows][kLongList]
+  KeepRow* head;            // [rows]
+  uint16_t* coarse;         // [rows][parts][kCoarse]
+  uint16_t* fine;           // [rows][parts][kBins]
 };
-__host__ __device__ static inline KeepWs keep_ws(void* ws, int64_t rows) {
+// About 1024 workgroups where there are many rows (more of them rank more lists), parts of 1024 tokens at least.
+static int keep_parts(int64_t rows, int n) {
+  int64_t most = 1024 / rows;
+  most = most < 16 ? 16 : (most > kParts ? kParts : most);
+  const int by_size = (n + 1023) / 1024;
+  return n > (1 << 18) ? kParts : (by_size < most ? by_size : (int)most);
+}
+static KeepWs keep_ws(void* ws, int64_t rows, int parts) {
   KeepWs k;
   k.list = reinterpret_cast<uint64_t*>(ws);
-  k.hist = reinterpret_cast<uint16_t*>(k.list + rows * kLongList);
-  k.head = reinterpret_cast<KeepRow*>(k.hist + rows * kParts * kBins);
+  k.head = reinterpret_cast<KeepRow*>(k.list + rows * kLongList);
+  k.coarse = reinterpret_cast<uint16_t*>(k.head + rows);
+  k.fine = k.coarse + rows * parts * kCoarse;
   return k;
 }
 struct KeepArgs {
@@ -182,11 +193,11 @@ struct KeepArgs {
   int64_t w_sb, w_sh;
   const int32_t* lens;
   int32_t* index;
-  int Hkv, n, keep, first, last;
+  int Hkv, n, keep, first, last, size;  // size: tokens of a part
 };
 struct Part {
   const float* weight;
-  int len, lo, hi, want, p0, p1, size;  // the part's tokens are p0 .. p1 - 1; size: of a part
+  int len, lo, hi, want, p0, p1, size;  // the part's tokens are p0 .. p1 - 1
   bool all_kept;
 };
 __device__ __forceinline__ Part part_of(const KeepArgs& A) {
@@ -196,7 +207,7 @@ __device__ __forceinline__ Part part_of(const KeepArgs& A) {
   p.len = A.lens != nullptr ? min(max(A.lens[b], 0), A.n) : A.n;
   p.all_kept = p.len <= A.keep;
   p.lo = A.first; p.hi = p.len - A.last; p.want = A.keep - A.first - A.last;
-  p.size = ((A.n + kParts - 1) / kParts + 255) / 256 * 256;
+  p.size = A.size;
   p.p0 = (int)min((int64_t)p.hi, p.lo + (int64_t)p.size * blockIdx.x);
   p.p1 = (int)min((int64_t)p.hi, (int64_t)p.p0 + p.size);
   return p;
@@ -249,74 +260,76 @@ __global__ __launch_bounds__(256) void keep_count_kernel(KeepArgs A, KeepWs ws) 
   __syncthreads();
   keys.each([&](int, uint32_t key, bool valid) { count_bins(hist, key, valid); });
   __syncthreads();
-  uint32_t* out = reinterpret_cast<uint32_t*>(ws.hist + ((int64_t)blockIdx.y * kParts + blockIdx.x) * kBins);
-  for (int i = threadIdx.x; i < kBins / 2; i += 256) out[i] = (uint32_t)hist[2 * i] | (uint32_t)hist[2 * i + 1] << 16;
+  const int64_t part = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  uint32_t* fine = reinterpret_cast<uint32_t*>(ws.fine + part * kBins);
+  for (int i = threadIdx.x; i < kBins / 2; i += 256) fine[i] = (uint32_t)hist[2 * i] | (uint32_t)hist[2 * i + 1] << 16;
+  // sums of 32: a quarter of one a thread
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) sum += hist[8 * threadIdx.x + i];
+  sum += __builtin_amdgcn_mov_dpp(sum, 0xb1, 0xf, 0xf, true);  // lanes of four
+  sum += __builtin_amdgcn_mov_dpp(sum, 0x4e, 0xf, 0xf, true);
+  if ((threadIdx.x & 3) == 0) ws.coarse[part * kCoarse + (threadIdx.x >> 2)] = (uint16_t)sum;
 }
 
 template <int PER>
 __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
-  __shared__ int chunk[4], sums[4], n_list;
+  __shared__ int sums[8][kCoarse], n_list;
+  __shared__ uint16_t fine[kParts][kFine];
   __shared__ uint32_t any4[4], all4[4];
-  __shared__ Bin found;
   const Part p = part_of(A);
   if (p.all_kept || p.want == 0) return;
-  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x;
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x, parts = gridDim.x;
   const int64_t row = blockIdx.y;
   const PartKeys<PER> keys(p);
-  // the row's bins 8 tid .. 8 tid + 7, and this part's
-  int sum[8], own[8];
-#pragma unroll
-  for (int i = 0; i < 8; i++) sum[i] = own[i] = 0;
+  // the bin, by sums of 32 first: a lane a bin
+  const uint16_t* coarse = ws.coarse + row * parts * kCoarse;
+  const int own = coarse[mine * kCoarse + l];
+  int sum = 0;
   {
-    const uint4* h = reinterpret_cast<const uint4*>(ws.hist + row * kParts * kBins) + tid;
-    uint4 x[kParts];
+    int v[kParts / 4];  // requested at once
 #pragma unroll
-    for (int c = 0; c < kParts; c++) x[c] = h[c * (kBins / 8)];
+    for (int k = 0; k < kParts / 4; k++) v[k] = w + 4 * k < parts ? coarse[(w + 4 * k) * kCoarse + l] : 0;
 #pragma unroll
-    for (int c = 0; c < kParts; c++) {
-      const uint32_t d[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const int v = (int)(i & 1 ? d[i >> 1] >> 16 : d[i >> 1] & 0xffffu);
-        sum[i] += v;
-        if (c == mine) own[i] = v;
-      }
-    }
+    for (int k = 0; k < kParts / 4; k++) sum += v[k];
   }
-  int total = 0;
-#pragma unroll
-  for (int i = 0; i < 8; i++) total += sum[i];
-  const int upto = wave_upto(total);
-  if (l == 63) chunk[w] = upto;
+  sums[w][l] = sum;
   if (tid == 0) n_list = 0;
   __syncthreads();
-  int below = upto - total;
+  sum = sums[0][l] + sums[1][l] + sums[2][l] + sums[3][l];
+  int upto = wave_upto(sum);
+  const int group = __builtin_ctzll(__ballot(upto >= p.want));  // want is at most the number of candidates
+  const int below_group = __builtin_amdgcn_readlane(upto - sum, group);
+  int sure = l < group ? own : 0;
+  __syncthreads();
+  {
+    const uint16_t* f = ws.fine + row * parts * kBins + group * kFine + (tid & 31);
+    int s = 0;
+    uint16_t v[kParts / 8];
 #pragma unroll
-  for (int k = 0; k < 4; k++)
-    if (k < w) below += chunk[k];
+    for (int k = 0; k < kParts / 8; k++) v[k] = (tid >> 5) + 8 * k < parts ? f[((tid >> 5) + 8 * k) * kBins] : (uint16_t)0;
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    if (below < p.want && p.want <= below + sum[i]) found = Bin{8 * tid + i, below, sum[i]};
-    below += sum[i];
+    for (int k = 0; k < kParts / 8; k++) {
+      fine[(tid >> 5) + 8 * k][tid & 31] = v[k];
+      s += v[k];
+    }
+    sums[tid >> 5][tid & 31] = s;
   }
   __syncthreads();
-  const Bin bin = found;
-  int sure = 0;
+  sum = 0;
+  if (l < kFine) {
 #pragma unroll
-  for (int i = 0; i < 8; i++)
-    if (8 * tid + i < bin.bin) sure += own[i];
-  sure = wave_upto(sure);
-  if (l == 63) sums[w] = sure;
-  // the parts' shares of the list
-  const uint16_t* at_bin = ws.hist + row * kParts * kBins + bin.bin;
-  int before = 0, listed = 0;
-#pragma unroll
-  for (int c = 0; c < kParts; c++) {
-    const int v = at_bin[c * kBins];
-    if (c < mine) before += v;
-    if (c == mine) listed = v;
+    for (int k = 0; k < 8; k++) sum += sums[k][l];
   }
-  uint64_t* list = ws.list + row * kLongList + before;
+  upto = below_group + wave_upto(sum);
+  const int at_fine = __builtin_ctzll(__ballot(upto >= p.want));
+  const Bin bin = {group * kFine + at_fine, __builtin_amdgcn_readlane(upto - sum, at_fine), __builtin_amdgcn_readlane(sum, at_fine)};
+  if (l < at_fine) sure += fine[mine][l];
+  sure = wave_upto(sure);  // lane 63's: tokens of the part in the bins before it
+  const int listed = l < parts ? fine[l][at_fine] : 0;  // of part l
+  const int listed_upto = wave_upto(listed);
+  const int of_mine = __builtin_amdgcn_readlane(listed, mine);
+  uint64_t* list = ws.list + row * kLongList + __builtin_amdgcn_readlane(listed_upto, mine) - of_mine;
   const bool write = bin.in <= kLongList;
   uint32_t any = 0u, all = ~0u;
   int n = 0;  // of the wave's tokens in the bin
@@ -340,11 +353,11 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
   const uint64_t bits = wave_or((uint64_t)any << 32 | ~all);
   if (l == 0) { any4[w] = (uint32_t)(bits >> 32); all4[w] = ~(uint32_t)bits; }
   __syncthreads();
-  if (tid == 0) {
+  if (tid == 63) {
     KeepRow* r = ws.head + row;
     if (mine == 0) { r->bin = bin.bin; r->rest = p.want - bin.below; r->in = bin.in; }
-    r->sure[mine] = sums[0] + sums[1] + sums[2] + sums[3];
-    r->listed[mine] = listed;
+    r->sure[mine] = sure;
+    r->listed[mine] = of_mine;
     r->any[mine] = any4[0] | any4[1] | any4[2] | any4[3];
     r->all[mine] = all4[0] & all4[1] & all4[2] & all4[3];
   }
@@ -352,33 +365,28 @@ __global__ __launch_bounds__(256) void keep_list_kernel(KeepArgs A, KeepWs ws) {
 
 template <int PER>
 __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
-  __shared__ uint64_t list[kLongList];
+  __shared__ uint64_t lds_list[kLdsList];
   __shared__ RankScratch rank;
   __shared__ int waves[4], more[4];
   const Part p = part_of(A);
-  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x;
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, mine = blockIdx.x, parts = gridDim.x;
   const int64_t row = blockIdx.y;
   int32_t* index = A.index + row * A.keep;
   if (p.all_kept) {
-    for (int i = 256 * mine + tid; i < A.keep; i += 256 * kParts) index[i] = i < p.len ? i : -1;
+    for (int i = 256 * mine + tid; i < A.keep; i += 256 * parts) index[i] = i < p.len ? i : -1;
     return;
   }
-  for (int i = 256 * mine + tid; i < A.first; i += 256 * kParts) index[i] = i;
-  for (int i = 256 * mine + tid; i < A.last; i += 256 * kParts) index[A.keep - A.last + i] = p.hi + i;
+  for (int i = 256 * mine + tid; i < A.first; i += 256 * parts) index[i] = i;
+  for (int i = 256 * mine + tid; i < A.last; i += 256 * parts) index[A.keep - A.last + i] = p.hi + i;
   if (p.want == 0) return;
   const PartKeys<PER> keys(p);
   const KeepRow* r = ws.head + row;
   const int bin = r->bin, rest = r->rest, in = r->in;
-  int at = A.first, bins_before = 0, bins_mine = 0;
-  uint32_t any = 0u, all = ~0u;
-#pragma unroll
-  for (int c = 0; c < kParts; c++) {
-    const int s = r->sure[c], b = r->listed[c];
-    if (c < mine) { at += s; bins_before += b; }
-    if (c == mine) bins_mine = b;
-    any |= r->any[c];
-    all &= r->all[c];
-  }
+  const int sure = l < mine ? r->sure[l] : 0, listed = l < parts ? r->listed[l] : 0;  // of part l
+  const uint64_t bits = wave_or(l < parts ? (uint64_t)r->any[l] << 32 | (uint32_t)~r->all[l] : 0ull);
+  const uint32_t any = (uint32_t)(bits >> 32), all = ~(uint32_t)bits;
+  int at = A.first + __builtin_amdgcn_readlane(wave_upto(sure), 63);
+  const int bins_mine = __builtin_amdgcn_readlane(listed, mine), bins_before = __builtin_amdgcn_readlane(wave_upto(listed), mine) - bins_mine;
   // Which tokens of the bin are kept: all; or, their keys alike, the first `rest` by place, of which this part has `mine_of_bin`; or those up
   // to `bound` in the list.
   const bool alike = any == all;
@@ -392,8 +400,12 @@ __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
   } else {
     int kept_before = 0;
     if (in <= kLongList) {
-      for (int i = tid; i < in; i += 256) list[i] = ws.list[row * kLongList + i];
-      __syncthreads();
+      const uint64_t* list = ws.list + row * kLongList;
+      if (in <= kLdsList) {
+        for (int i = tid; i < in; i += 256) lds_list[i] = list[i];
+        __syncthreads();
+        list = lds_list;
+      }
       bound = smallest_bound<256>(rest, [&](auto fn) {
         for (int i = tid; i < in; i += 256) fn(list[i]);
       }, &rank);
@@ -470,7 +482,7 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(int Hkv, int keep, hs_
 
 size_t hs_keep_ws_bytes(int64_t rows, int n) {
   if (n <= HS_KEEP_SHORT) return 0;
-  return (size_t)rows * (kLongList * sizeof(uint64_t) + (size_t)kParts * kBins * sizeof(uint16_t) + sizeof(KeepRow));
+  return (size_t)rows * (kLongList * sizeof(uint64_t) + sizeof(KeepRow) + (size_t)keep_parts(rows, n) * (kCoarse + kBins) * sizeof(uint16_t));
 }
 
 hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
@@ -481,17 +493,20 @@ hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, c
   } else if (n <= HS_KEEP_SHORT) {
     hipLaunchKernelGGL((keep_select_kernel<1024>), dim3(rows), dim3(1024), 0, st, Hkv, n, weight, w_sb, w_sh, lens, keep, first, last, index);
   } else {
-    const KeepArgs A{weight, w_sb, w_sh, lens, index, Hkv, n, keep, first, last};
-    const KeepWs k = keep_ws(ws, rows);
-    const dim3 grid(kParts, rows);
+    const int parts = keep_parts(rows, n), size = ((n + parts - 1) / parts + 255) / 256 * 256;  // at most 2^20 / 64: counts fit 16 bits
+    const KeepArgs A{weight, w_sb, w_sh, lens, index, Hkv, n, keep, first, last, size};
+    const KeepWs k = keep_ws(ws, rows, parts);
+    const dim3 grid(parts, rows);
 #define HS_KEEP(PER_)                                                                  \
   do {                                                                                 \
     hipLaunchKernelGGL((keep_count_kernel<PER_>), grid, dim3(256), 0, st, A, k);       \
     hipLaunchKernelGGL((keep_list_kernel<PER_>), grid, dim3(256), 0, st, A, k);        \
     hipLaunchKernelGGL((keep_take_kernel<PER_>), grid, dim3(256), 0, st, A, k);        \
   } while (0)
-    if (n <= kParts * 256 * 8) HS_KEEP(8);
-    else if (n <= kParts * 256 * 32) HS_KEEP(32);
+    if (size <= 256 * 4) HS_KEEP(4);
+    else if (size <= 256 * 8) HS_KEEP(8);
+    else if (size <= 256 * 16) HS_KEEP(16);
+    else if (size <= 256 * 32) HS_KEEP(32);
     else HS_KEEP(0);
 #undef HS_KEEP
   }

@@ -570,6 +570,16 @@ def test_keep_tokens_of_views_and_long_rows():
     _check_keep(sh, K, V, w, 5000, 64, 256, None)
 
 
+@gpu
+@pytest.mark.parametrize("n,alike", [(600001, False), (600001, True), (1 << 20, False)])
+def test_keep_tokens_of_the_longest_rows(n, alike):
+    sh = hb.make_shape(1, 1, 1, TILE)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    K = torch.randn((1, 1, n, D), generator=g, device="cuda").bfloat16()
+    w = torch.full((1, 1, n), 3.0, device="cuda") if alike else torch.rand((1, 1, n), generator=g, device="cuda")
+    _check_keep(sh, K, K, w, 1000, 4, 32, None)
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # together, captured, refused
 # ---------------------------------------------------------------------------------------------------------------------
