@@ -420,6 +420,7 @@ HS_API int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, co
  * A query whose LSE is not finite (one that saw nothing; one the caller leaves out by setting its LSE to -inf) weighs nothing.
  *   Q     [B, Hq, Lq, D], any Lq >= 1; query i stands at q_start + i and sees what hs_prefill_attn_at lets it see (0 <= q_start,
  *         q_start + Lq <= L if causal, else q_start is not looked at)
+ *         (HS_EUNSUPPORTED where the queries and LSEs of 32 positions of a group's heads lie further than 4 GiB apart)
  *   LSE   fp32, element strides lse_strides[2] = {batch, head} (NULL: contiguous [B, Hq, Lq]), queries contiguous
  *   mass  fp32 [B, Hkv, L / 64], or with per_token [B, Hkv, L]; mass_in NULL: zeros (as with decay 0, when it is not read); mass_out may be
  *         mass_in.  Tiles that are SKIP get decay mass_in.
@@ -443,7 +444,8 @@ HS_API int hs_attn_mass_workspace_bytes(const hs_shape* shape, int32_t Lq, int c
  * Nothing is copied but what has to move: the used slots of a pool are 0 .. n - 1 again afterwards, because the remaining tiles whose slots
  * are n or above move, in ascending order, into the freed slots below n, in ascending order (at most as many moves as dropped tiles),
  * so hs_append_tile goes on from there.  Slots from n on keep their bytes.  Every held tile's slots have to be distinct and 0 .. n - 1
- * in their pool, as all calls of this library leave them.  kv->uniform must be 0.  L / 64 <= 65536.
+ * in their pool, as all calls of this library leave them.  kv->uniform must be 0, and 0 in every later call on this cache (calls captured
+ * with the promise are not valid any more).  L / 64 <= 65536.
  * workspace: hs_workspace_bytes(op 4), 4-byte aligned, not shared between two calls in flight; no initial content. */
 HS_API int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* mass, int32_t keep, const int32_t* keeps, int32_t first,
                    int32_t last, void* workspace, void* stream);

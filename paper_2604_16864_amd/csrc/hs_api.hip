@@ -697,17 +697,19 @@ int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale
   hs_vec_view q;
   rc = view_of(Q, shape->B, shape->Hq, Lq, false, &q);
   if (rc != HS_OK) return rc;
+  // strides of axes of size 1 are not looked at
+  const int64_t l_sb = shape->B == 1 ? 0 : (lse_strides != nullptr ? lse_strides[0] : (int64_t)shape->Hq * Lq);
+  const int64_t l_sh = shape->Hq == 1 ? 0 : (lse_strides != nullptr ? lse_strides[1] : Lq);
+  if (l_sb < 0 || l_sh < 0) return HS_EINVAL;
   // the kernel for many queries reads the queries of 32 / G positions and G heads by 32-bit byte offsets
-  const int64_t l_sh_in = lse_strides != nullptr ? lse_strides[1] : Lq;
-  if (l_sh_in < 0 || (lse_strides != nullptr && lse_strides[0] < 0)) return HS_EINVAL;
-  if ((double)q.st * 62.0 + (double)q.sh * 14.0 >= 4294967040.0 || (double)l_sh_in * 28.0 >= 4294967040.0) return HS_EUNSUPPORTED;
+  if ((double)q.st * 62.0 + (double)q.sh * 14.0 >= 4294967040.0 || (double)l_sh * 28.0 >= 4294967040.0) return HS_EUNSUPPORTED;
   hs_mass_args a = {};
   a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, causal != 0, per_token != 0);
+  if ((int64_t)a.n_ranges * shape->Hkv * (shape->L / HS_BT) > INT32_MAX) return HS_EUNSUPPORTED;  // the grid
   if (a.n_ranges > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
   a.q = q.p; a.q_sb = q.sb; a.q_sh = q.sh; a.q_st = q.st;
   a.lse = LSE;
-  a.l_sb = lse_strides != nullptr ? lse_strides[0] : (int64_t)shape->Hq * Lq;
-  a.l_sh = lse_strides != nullptr ? lse_strides[1] : Lq;
+  a.l_sb = l_sb; a.l_sh = l_sh;
   a.tail_k = (const uint16_t*)tail_k; a.tail_lens = tail_lens; a.tail_tiles = tail_tiles; a.tail_len = tail_len; a.tail_tile = tail_tile;
   a.in = mass_in; a.out = mass_out; a.ws = (float*)workspace;
   a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.T = shape->L / HS_BT;
@@ -748,8 +750,9 @@ int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, co
   if (rc != HS_OK) return rc;
   rc = view_of(V, shape->B, shape->Hkv, n_tokens, false, &v);
   if (rc != HS_OK) return rc;
-  const int64_t w_sb = weight_strides != nullptr ? weight_strides[0] : (int64_t)shape->Hkv * n_tokens;
-  const int64_t w_sh = weight_strides != nullptr ? weight_strides[1] : n_tokens;
+  const int64_t w_sb = shape->B == 1 ? 0 : (weight_strides != nullptr ? weight_strides[0] : (int64_t)shape->Hkv * n_tokens);
+  const int64_t w_sh = shape->Hkv == 1 ? 0 : (weight_strides != nullptr ? weight_strides[1] : n_tokens);
+  if (w_sb < 0 || w_sh < 0) return HS_EINVAL;
   const hipError_t e = hs_launch_keep(shape->B, shape->Hkv, n_tokens, k, v, weight, w_sb, w_sh, lens, keep, first, last, (uint16_t*)K_out,
                                       (uint16_t*)V_out, index, workspace, (hipStream_t)stream);
   return e != hipSuccess ? hip_fail(e) : HS_OK;

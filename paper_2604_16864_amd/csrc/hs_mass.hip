@@ -100,7 +100,7 @@ __device__ __forceinline__ void put(const hs_mass_args& A, int64_t row, int t, f
 }
 
 // One query per head.  HBM-bound on the packed keys: a wave takes a tile, reads each of its bytes once, straight into operand registers.
-// Columns are the group's heads.
+// Columns are the group's heads.  8 rows of 512 2:4 tiles (37.8 MB) take 7.1 us, 64 rows of 2048 with half of them held (606 MB) 93 us, 6.5 TB/s.
 template <bool F16, int KM>
 __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_dev kv, float scale_log2) {
   const int tid = threadIdx.x, l = tid & 63, a = l >> 4, c = l & 15;
@@ -154,6 +154,12 @@ __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_de
 }
 
 // ---- many queries ----
+// What bounds it: per score one fused multiply-add, one exponential (two issue slots) and one addition of the vector ALU, 77 % of whose time
+// they take (32 columns and a tile: 814 clocks, of which 552 are these and the issue of 10 matrix instructions; the matrix pipe is 39 %
+// busy), at 2.1 GHz, which the power limit holds: a 16K prompt, 32 heads, 2:4 keys 804 us.  Measured beside it: one set of scores and one or two
+// more waves per SIMD instead of products beside exponentials 850 (dense keys, per tile 496 / 515); two tiles a wave, for half of the
+// reads of LDS and L2, 1005 (2 waves per SIMD instead of 3); the vector ALU's own order, products first, 1155.
+//
 // The queries of a kv head's group pass by in blocks of 32 columns (32 / G queries, the group's G heads of each side by side), the B operand of
 // the 32x32 matrix instructions, staged in LDS for the workgroup's four waves, which hold a tile of 64 tokens each.
 //
