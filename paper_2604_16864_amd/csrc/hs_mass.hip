@@ -156,7 +156,8 @@ __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_de
 // ---- many queries ----
 // What bounds it: per score one fused multiply-add, one exponential (two issue slots) and one addition of the vector ALU, 77 % of whose time
 // they take (32 columns and a tile: 814 clocks, of which 552 are these and the issue of 10 matrix instructions; the matrix pipe is 39 %
-// busy), at 2.1 GHz, which the power limit holds: a 16K prompt, 32 heads, 2:4 keys 804 us.  Measured beside it: one set of scores and one or two
+// busy), at 2.1 GHz, which the power limit holds: a 16K prompt, 32 heads, 2:4 keys 800 us; 4096 queries on 16K tokens, 2:4 keys per tile 366, per
+// token 396, dense keys 484 and 497.  A barrier every two blocks, and the columns' LSE once, are worth 1 to 2 % of it.  Measured beside it: one set of scores and one or two
 // more waves per SIMD instead of products beside exponentials 850 (dense keys, per tile 496 / 515); two tiles a wave, for half of the
 // reads of LDS and L2, 1005 (2 waves per SIMD instead of 3); the vector ALU's own order, products first, 1155.
 //
@@ -296,8 +297,8 @@ __device__ __forceinline__ void lds_load4(uint32_t base, const void* p, uint32_t
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(base), "v"(off), "s"((uint64_t)p) : "memory", "m0");
 }
 
-constexpr int kStages = 3;                        // a block is requested two blocks ahead
-constexpr int kStageBytes = 8 * 1024 + 4 * 256;   // 32 columns of 256 bytes, and a copy of the columns' LSE for each wave
+constexpr int kStages = 4;                        // two blocks are worked on while the next two are on their way
+constexpr int kStageBytes = 8 * 1024 + 256;       // 32 columns of 256 bytes, and the columns' LSE (twice)
 constexpr int kGroup = 4;                         // tiles of a workgroup
 constexpr int kAhead = 2;                         // pairs of exponentials in front of a block's first products
 
@@ -409,23 +410,24 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
       }
       lds_load16(at + 2048 * w, q, o0);
       lds_load16(at + 2048 * w + 1024, q, o1);
-      lds_load4(at + 8192 + 256 * w, ls, ol);
+      if (w == (blk & 3)) lds_load4(at + 8192, ls, ol);
       q += q_step;
       ls += Q;
     };
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // the tile's own loads: only the requests are counted from here on
     request(0, 0);
     if (n > 1) request(1, 1);
 
     int stage = kStages - 1;  // of the block last waited for
-    // Waits for block blk (each one once, in order) and requests the one two further on, into the stage that every wave has left.
+    // Waits for block blk (each one once, in order): for two at a time, and the two behind them are requested, into the stages that every wave
+    // has left.
     auto wait_for = [&](int blk) {
-      if (blk + 1 < n) asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (blk + 2 < n) request(blk + 2, stage);
-      stage = stage == kStages - 1 ? 0 : stage + 1;
+      stage = (stage + 1) & (kStages - 1);
+      if (blk & 1) return;
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (blk + 2 < n) request(blk + 2, stage ^ 2);
+      if (blk + 3 < n) request(blk + 3, (stage ^ 2) + 1);
     };
-    const uint32_t my_column = 256 * r + 16 * (hi ^ (r & 15)), my_lse = 8192 + 256 * w + 4 * l;
+    const uint32_t my_column = 256 * r + 16 * (hi ^ (r & 15)), my_lse = 8192 + 4 * l;
     auto fetch = [&](uint4 (&x)[8], float& lse) {
       const uint32_t at = stage * kStageBytes + my_column;
 #pragma unroll
