@@ -553,7 +553,13 @@ __global__ __launch_bounds__(256) void mass_join_kernel(hs_mass_args A, int64_t 
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   float sum = 0.f;
-  for (int r = 0; r < A.n_ranges; r++) sum += A.ws[r * n + i];
+  for (int r0 = 0; r0 < A.n_ranges; r0 += 16) {  // requested 16 at a time
+    float x[16];
+#pragma unroll
+    for (int k = 0; k < 16; k++) x[k] = r0 + k < A.n_ranges ? A.ws[(r0 + k) * n + i] : 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; k++) sum += x[k];
+  }
   A.out[i] = faded(A, i) + sum;
 }
 
