@@ -499,6 +499,59 @@ def test_evict_the_longest_row():
     _check_evict(sh, kv, maps, mass, 700, 1, 4, lambda: hb.evict_tiles(sh, kv, torch.from_numpy(mass).cuda(), 700, first=1, last=4))
 
 
+@gpu
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("sk,sv", [(1.0, 1.0), (0.5, 1.0), (0.0, 0.5)])
+def test_a_cache_after_eviction_is_a_cache(sk, sv, dtype):
+    """Unpacking, attention, re-packing, mass and a further eviction see the cache that packing only the remaining tiles would have made."""
+    B, Hkv, G, L = 2, 2, 4, 1536
+    T, t = L // TILE, TYPES[dtype]
+    g = _gen(31)
+    K, V = (torch.randn((B, Hkv, L, D), generator=g).to(t).cuda() for _ in range(2))
+    sh = hb.make_shape(B, Hkv * G, Hkv, L, dtype=t)
+    kv = hb.compress_kv(sh, hb.make_policy(sparse_frac_k=sk, sparse_frac_v=sv), K, V)
+    K0, V0 = hb.unpack_kv(sh, kv)
+    states = [np.where(m > 0, hb.DENSE, np.where(m < 0, hb.SPARSE24, hb.SKIP)).astype(np.int8) for m in (kv.k_map.cpu().numpy(), kv.v_map.cpu().numpy())]
+    mass = torch.rand((B, Hkv, T), generator=g)
+    hb.evict_tiles(sh, kv, mass.cuda(), 9, first=1, last=2)
+    gone = (kv.k_map == 0).cpu()
+    assert bool(((~gone).sum(-1) == 9).all()) and torch.equal(gone, (kv.v_map == 0).cpu())
+    keep = (~gone).repeat_interleave(TILE, -1).cuda()  # chooses rows; a product with 0 would make -0 of a negative value
+    Ku, Vu = hb.unpack_kv(sh, kv)
+    assert torch.equal(_bits(Ku[keep]), _bits(K0[keep])) and torch.equal(_bits(Vu[keep]), _bits(V0[keep]))
+    for s in states:
+        s[gone.numpy()] = hb.SKIP
+    pol = hb.make_policy(state_k=states[0], state_v=states[1])
+    fresh = hb.PackedKV(sh, kv.counts, "cuda")
+    hb.compress_kv(sh, pol, K, V, out=fresh)
+    hb.check_state_flag(pol)
+    q = torch.randn((B, Hkv * G, 128, D), generator=g).to(t).cuda()
+    for a, b in zip(hb.prefill_attn(sh, q, kv), hb.prefill_attn(sh, q, fresh)):
+        assert torch.equal(a, b)
+    d = q[:, :, 0].contiguous()
+    for a, b in zip(hb.decode_attn(sh, d, kv), hb.decode_attn(sh, d, fresh)):
+        assert torch.equal(a, b)
+    lse = torch.full((B, Hkv * G, 128), 6.0, device="cuda")
+    assert torch.equal(hb.attn_mass(sh, q, lse, kv), hb.attn_mass(sh, q, lse, fresh))
+    one, other = (hb.recompress_kv(sh, x, hb.make_policy(dense_first_tiles=1, dense_last_tiles=1)) for x in (kv, fresh))
+    assert torch.equal(one.k_map, other.k_map) and torch.equal(one.v_map, other.v_map)
+    for a, b in zip(hb.unpack_kv(sh, one), hb.unpack_kv(sh, other)):
+        assert torch.equal(_bits(a[keep]), _bits(b[keep]))
+    # the last tile, dropped from every row by a mass of its own, comes back through an append
+    lightest = torch.ones_like(mass)
+    lightest[..., T - 1] = 0
+    hb.evict_tiles(sh, kv, lightest.cuda(), 8)
+    assert bool((kv.k_map[..., T - 1] == 0).all()) and bool(((kv.k_map != 0).sum(-1) == 8).all())
+    over = torch.zeros(1, dtype=torch.int32, device="cuda")
+    if sk == sv == 1.0:  # pools of one kind have the room in every row
+        hb.append_tile(sh, kv, T - 1, K[:, :, -TILE:], V[:, :, -TILE:], overflow=over)
+        assert int(over) == 0
+        for a, b in zip(hb.unpack_kv(sh, kv), (K0, V0)):
+            assert torch.equal(_bits(a[:, :, -TILE:]), _bits(b[:, :, -TILE:]))
+    hb.evict_tiles(sh, kv, mass.cuda(), 4)
+    assert int((kv.k_map != 0).sum(-1).max()) == 4
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # choice of tokens
 # ---------------------------------------------------------------------------------------------------------------------
