@@ -418,7 +418,7 @@ HS_API int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, co
  *              exp(scale q_i . k_j - LSE_i),
  * the column sums of the softmax that prefill or decode attention over this cache computed, from the LSE that it returned (natural log).
  * A query whose LSE is not finite (one that saw nothing; one the caller leaves out by setting its LSE to -inf) weighs nothing.
- *   Q     [B, Hq, Lq, D], any Lq >= 1; query i stands at q_start + i and sees what hs_prefill_attn_at lets it see (0 <= q_start,
+ *   Q     [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i and sees what hs_prefill_attn_at lets it see (0 <= q_start,
  *         q_start + Lq <= L if causal, else q_start is not looked at)
  *         (HS_EUNSUPPORTED where the queries and LSEs of 32 positions of a group's heads lie further than 4 GiB apart)
  *   LSE   fp32, element strides lse_strides[2] = {batch, head} (NULL: contiguous [B, Hq, Lq]), queries contiguous
@@ -457,7 +457,7 @@ HS_API int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* m
  *   weight    device fp32, element strides weight_strides[2] = {batch, head} (NULL: contiguous [B, Hkv, n_tokens]), tokens contiguous
  *   index     device int32 [B, Hkv, keep]: the tokens kept
  * A row of fewer than `keep` tokens keeps them all; the rest of its outputs is 0 and its indices -1.  keep >= first + last,
- * keep >= 1, n_tokens <= 2^20.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  Outputs overlap neither
+ * 1 <= keep <= 2^30, n_tokens <= 2^20.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  Outputs overlap neither
  * inputs nor each other.  workspace: hs_workspace_bytes(op 5, n_tokens), 16-byte aligned (NULL where that is 0), not shared between
  * two calls in flight; no initial content. */
 HS_API int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,

@@ -672,6 +672,7 @@ int hs_attn_mass_workspace_bytes(const hs_shape* shape, int32_t Lq, int causal, 
   const int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (Lq < 1 || bytes == nullptr) return HS_EINVAL;
+  if (Lq > 1 << 30) return HS_EUNSUPPORTED;
   const int T = shape->L / HS_BT;
   const int n = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, T, Lq, causal != 0, per_token != 0);
   *bytes = n > 1 ? (size_t)n * shape->B * shape->Hkv * T * (per_token != 0 ? HS_BT : 1) * sizeof(float) : 0;
@@ -687,6 +688,7 @@ int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale
   rc = check_kv(shape, kv);
   if (rc != HS_OK) return rc;
   if (Lq < 1 || Q == nullptr || LSE == nullptr || mass_out == nullptr) return HS_EINVAL;
+  if (Lq > 1 << 30) return HS_EUNSUPPORTED;
   if (((uintptr_t)LSE | (uintptr_t)mass_in | (uintptr_t)mass_out) & 3u) return HS_EINVAL;
   if (causal && (q_start < 0 || Lq > shape->L || q_start > shape->L - Lq)) return HS_EINVAL;
   if (!(scale >= 0.f) || !(decay >= 0.f) || !(decay < INFINITY)) return HS_EINVAL;
@@ -741,7 +743,7 @@ int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, co
   int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (n_tokens < 1 || K == nullptr || V == nullptr || weight == nullptr || K_out == nullptr || V_out == nullptr || index == nullptr) return HS_EINVAL;
-  if (n_tokens > 1 << 20) return HS_EUNSUPPORTED;
+  if (n_tokens > 1 << 20 || keep > 1 << 30) return HS_EUNSUPPORTED;
   if ((((uintptr_t)K_out | (uintptr_t)V_out) & 15u) || (((uintptr_t)weight | (uintptr_t)index) & 3u)) return HS_EINVAL;
   if (keep < 1 || first < 0 || last < 0 || (int64_t)first + last > keep) return HS_EINVAL;
   if (((uintptr_t)workspace & 15u) || (workspace == nullptr && hs_keep_ws_bytes((int64_t)shape->B * shape->Hkv, n_tokens) != 0)) return HS_EINVAL;

@@ -891,6 +891,17 @@ def test_refusals_on_the_host():
         assert keep(**bad) == rc, bad
 
 
+def test_refusals_of_counts_near_the_end_of_32_bits():
+    """Queries that all lie at one address (stride 0) may be as many as an int counts, and so may rows of padding: what the kernels' sums cannot hold is refused."""
+    L, sh = hb.lib(), hb.make_shape(1, 8, 2, 256)
+    one, kv, size = C.byref(hb.HsView(4096, 0, D, 0)), C.byref(hb.HsKV(k_map=4096, v_map=4096)), C.c_size_t(0)
+    for Lq in ((1 << 30) + 1, 2 ** 31 - 1):
+        assert L.hs_attn_mass(C.byref(sh), Lq, 0, 0.0, 0, one, 4096, None, kv, None, 0, None, 0, None, 0, 1.0, None, 4096, 4096, None) == -2
+        assert L.hs_attn_mass_workspace_bytes(C.byref(sh), Lq, 0, 0, C.byref(size)) == -2
+        assert L.hs_keep_tokens(C.byref(sh), 100, one, one, 4096, None, None, Lq, 0, 0, 4096, 4096, 4096, 4096, None) == -2
+    assert L.hs_attn_mass_workspace_bytes(C.byref(sh), 1 << 30, 0, 0, C.byref(size)) == 0
+
+
 def test_refusals_of_the_binding():
     """Tensors that are not where or what the call takes."""
     sh, rope = hb.make_shape(1, 4, 2, 128), hb.make_rope()
