@@ -157,9 +157,8 @@ __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_de
 // What bounds it: per score one fused multiply-add, one exponential (two issue slots) and one addition of the vector ALU, 77 % of whose time
 // they take (32 columns and a tile: 814 clocks, of which 552 are these and the issue of 10 matrix instructions; the matrix pipe is 39 %
 // busy), at 2.1 GHz, which the power limit holds: a 16K prompt, 32 heads, 2:4 keys 800 us; 4096 queries on 16K tokens, 2:4 keys per tile 366, per
-// token 396, dense keys 484 and 497.  A barrier every two blocks, and the columns' LSE once, are worth 1 to 2 % of it.  Measured beside it: one set of scores and one or two
-// more waves per SIMD instead of products beside exponentials 850 (dense keys, per tile 496 / 515); two tiles a wave, for half of the
-// reads of LDS and L2, 1005 (2 waves per SIMD instead of 3); the vector ALU's own order, products first, 1155.
+// token 396, dense keys 460 and 481.  A barrier every two blocks, and the columns' LSE once, are worth 1 to 2 % of it.  Measured beside it: two tiles a wave, for half
+// of the reads of LDS and L2, 1005 (2 waves per SIMD instead of 3); the scheduler's own order, products first, 1155.
 //
 // The queries of a kv head's group pass by in blocks of 32 columns (32 / G queries, the group's G heads of each side by side), the B operand of
 // the 32x32 matrix instructions, staged in LDS for the workgroup's four waves, which hold a tile of 64 tokens each.
@@ -301,12 +300,17 @@ constexpr int kStages = 4;                        // two blocks are worked on wh
 constexpr int kStageBytes = 8 * 1024 + 256;       // 32 columns of 256 bytes, and the columns' LSE (twice)
 constexpr int kGroup = 4;                         // tiles of a workgroup
 constexpr int kAhead = 2;                         // pairs of exponentials in front of a block's first products
+// Products of a block beside the exponentials of the one before (two sets of scores), or one set and, for the registers that this frees, 3 waves per
+// SIMD instead of 2 (dense keys).  us, beside / one set: dense keys per tile, 4096 queries on 16K tokens 470 / 460, 512 on 4 x 4K 85 / 81, a 2K prompt
+// 39 / 33, 100 queries on 32K 41 / 40; per token 481 / 592 (registers spilled).  2:4 keys, 3 waves either way, per tile: 4096 queries 366 / 362, 128 on 32K
+// 37.8 / 36.6, a 16K prompt 802 / 817, a 2K one 31 / 32.5; per token 423 / 432, a 16K prompt 918 / 957.
+constexpr bool beside(bool token, bool dense) { return token || !dense; }
 
 // A block's 32 columns lie in LDS one after the other, the 16-byte chunks of column r exchanged by c -> c ^ (r & 15): loads from memory are of
 // whole 256-byte vectors, 4 to an instruction (as matrix operands, 16 bytes of 64 vectors to an instruction, they cost 500 clocks a
 // block), and reads of one chunk of 32 columns touch every bank alike.
 template <bool F16, bool TOKEN, bool DENSE>
-__global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev kv, float scale_log2) {
+__global__ __launch_bounds__(256, beside(TOKEN, DENSE) ? 2 : 3) void mass_kernel(hs_mass_args A, hs_kv_dev kv, float scale_log2) {
   __shared__ __attribute__((aligned(256))) uint8_t lds[kStages * kStageBytes];
   const int tid = threadIdx.x, l = tid & 63, hi = l >> 5, r = l & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -491,6 +495,14 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
       sum(30); sum(31);
       if (!TOKEN) tile_sum += (part[0] + part[1]) + (part[2] + part[3]);
     };
+    // the same scores without the products, tiles only
+    auto weigh_all = [&](const f32x16_t (&s)[2], float lse) {
+      const float lse2 = lse * kLog2e;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 32; e++) part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -lse2));
+      tile_sum += (part[0] + part[1]) + (part[2] + part[3]);
+    };
     f32x16_t s0[2], s1[2];
     float lse0, lse1;
     const int n_steady = min(n, n_whole) - 1;  // blocks that have a whole one behind them
@@ -503,7 +515,7 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
 #pragma unroll
         for (int i = 0; i < KTile32<F16, DENSE>::kSteps; i++) tile.step(i, x, s0);
       }
-      if (blk >= full) {
+      if (beside(TOKEN, DENSE) && blk >= full) {
         for (;;) {
           if (blk >= n_steady || !all_count(lse0)) break;
           wait_for(blk + 1);
@@ -517,6 +529,11 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(hs_mass_args A, hs_kv_dev 
           both(s0, lse0, s1, lse1);
           blk++;
         }
+      }
+      if (!beside(TOKEN, DENSE) && blk >= full && blk < n_whole && all_count(lse0)) {
+        weigh_all(s0, lse0);
+        blk++;
+        continue;
       }
       weigh_seen(s0, lse0, blk);
       blk++;
