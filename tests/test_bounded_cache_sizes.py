@@ -1,0 +1,117 @@
+"""The operators around a bounded cache at the sizes where another kernel or another share of the work is chosen: held tiles numbered by the workgroups
+(attention mass), rows in parts of every length (choice of tokens), counts near what a launch holds.  Plain forms in 64 bits on the device."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_16864_amd import binding as hb
+
+gpu = pytest.mark.gpu
+D, TILE = 128, 64
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def _bits(t):
+    return t.detach().contiguous().view(torch.int16)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# attention mass of many queries where tiles may be missing
+# ---------------------------------------------------------------------------------------------------------------------
+def _states(kinds, B, Hkv, T, g):
+    """Tile states: row 0 holds nothing, row 1 one tile, row 2 (or the last) all of them, the others a number that is no multiple of 4."""
+    s = torch.zeros((B * Hkv, T), dtype=torch.int8)
+    for r in range(B * Hkv):
+        n = {0: 0, 1: 1, 2: T}.get(r, max(1, (2 * T // 5) // 4 * 4 + 1 + r % 3)) if B * Hkv > 2 else (T // 4 // 4 * 4 + 3, T)[r]
+        at = torch.randperm(T, generator=g)[:min(n, T)]
+        s[r, at] = torch.tensor(kinds, dtype=torch.int8)[torch.randint(0, len(kinds), (len(at),), generator=g)]
+    s = s.reshape(B, Hkv, T).numpy()
+    v = np.where(s == hb.SKIP, hb.SKIP, hb.SPARSE24).astype(np.int8)
+    return s, v
+
+
+def _mass_64(Q, K, lse, held, causal, q_start):
+    """What each token gets [B, Hkv, L], and the error of the scores' way there: a score is a sum of D exact products (D + 1 roundings of
+    the sum of magnitudes at most), the argument of the exponential is off by 4 2^-24 of each of its two parts, an exponential by 4 2^-24."""
+    B, Hq, Lq, _ = Q.shape
+    Hkv, L = K.shape[1], K.shape[2]
+    G, e, scale = Hq // Hkv, 2.0 ** -24, 1 / math.sqrt(D)
+    out, tol = (torch.zeros((B, Hkv, L), dtype=torch.float64, device="cuda") for _ in range(2))
+    at = torch.arange(L, device="cuda")
+    for b in range(B):
+        for hq in range(Hq):
+            h = hq // G
+            seen_tile = held[b, h].repeat_interleave(TILE)
+            for i in range(0, Lq, 512):
+                q, ls = Q[b, hq, i:i + 512].double(), lse[b, hq, i:i + 512].double()[:, None]
+                s = torch.matmul(q, K[b, h].double().t()) * scale
+                size = torch.matmul(q.abs(), K[b, h].double().abs().t()) * scale
+                seen = seen_tile & torch.isfinite(ls)
+                if causal:
+                    seen = seen & (at <= q_start + i + torch.arange(len(q), device="cuda")[:, None])
+                p = torch.where(seen, torch.exp(s - ls), 0.0)
+                out[b, h] += p.sum(0)
+                tol[b, h] += torch.where(seen, p * ((D + 1) * e * size + 4 * e * (s.abs() + ls.abs()) + 4 * e), 0.0).sum(0)
+    return out, tol
+
+
+@gpu
+@pytest.mark.parametrize("kinds", [(hb.SPARSE24,), (hb.DENSE,), (hb.DENSE, hb.SPARSE24)], ids=["2:4", "dense", "mixed"])
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("B,Hkv,G,T,Lq,causal,ranges", [
+    (2, 2, 4, 601, 60, True, 1),        # 604 workgroups, a row's last group of one tile
+    (1, 1, 3, 2051, 77, False, 1),      # 513, and more tiles than one walk over the map looks at; 32 columns are 10 queries and 2 to spare
+    (1, 2, 8, 2050, 31, True, 1),       # a second walk of two tiles
+    (2, 2, 4, 21, 1300, True, 22),      # 528 in ranges of 7 blocks, queries before the first tile's end
+    (1, 3, 1, 130, 2000, False, 6),     # 594 in ranges of 10 blocks of 32 queries of one head
+    (4, 1, 4, 299, 4000, True, 28),     # 8400 in ranges of 17 blocks
+])
+def test_mass_where_held_tiles_are_numbered(B, Hkv, G, T, Lq, causal, ranges, dtype, kinds):
+    """Calls of more than 512 workgroups, in one range of the queries and in several: rows that hold nothing, one tile, some and all; every element of
+    the output and of the workspace is written, missing tiles get what they had."""
+    L, t = T * TILE, TYPES[dtype]
+    sh = hb.make_shape(B, Hkv * G, Hkv, L, dtype=t)
+    g, gd = torch.Generator().manual_seed(T + Lq), torch.Generator(device="cuda").manual_seed(T + Lq)
+    s, v = _states(kinds, B, Hkv, T, g)
+    K = torch.randn((B, Hkv, L, D), generator=gd, device="cuda").to(t)
+    kv = hb.compress_kv(sh, hb.make_policy(state_k=s, state_v=v), K, K)
+    assert not kv.uniform
+    held = kv.k_map != 0
+    assert torch.equal(held.cpu(), torch.from_numpy(s != hb.SKIP))
+    Ku, _ = hb.unpack_kv(sh, kv)
+    Q = torch.randn((B, Hkv * G, Lq, D), generator=gd, device="cuda").to(t)
+    lse = torch.randn((B, Hkv * G, Lq), generator=gd, device="cuda") + math.log(L)
+    lse[:, :, Lq // 3] = -math.inf                       # queries that do not count, one in every head
+    q_start = L - Lq
+    if not causal:
+        q_start = 0
+    elif Lq > TILE:
+        q_start = min(q_start, 40)                       # what lies behind the last query is seen by none
+    want, tol = _mass_64(Q, Ku, lse, held, causal, q_start)
+    for per_token in (False, True):
+        need = hb.attn_mass_workspace_bytes(sh, Lq, causal, per_token)
+        sizes = (B, Hkv, L if per_token else T)
+        out_bytes = 4 * B * Hkv * sizes[2]
+        n_ranges = max(1, need // out_bytes)
+        # tokens: as many as 64 MiB hold
+        assert n_ranges == min(ranges, max(1, (64 << 20) // out_bytes)) and n_ranges * B * Hkv * ((T + 3) // 4) > 512
+        w, e = (want, tol) if per_token else (x.reshape(B, Hkv, T, TILE).sum(-1) for x in (want, tol))
+        # terms of a sum are added to it one after the other a block of queries and a range of them at a time, before that and after it by at most 20 more
+        depth = (Lq + 32 // G - 1) // (32 // G) + 20
+        e = e + depth * 2.0 ** -24 * w
+        before = torch.rand(sizes, generator=gd, device="cuda")
+        ws = torch.full((max(16, need),), 0xff, dtype=torch.uint8, device="cuda")          # NaN
+        for decay in (0.0, 0.75):
+            got = hb.attn_mass(sh, Q, lse, kv, mass=before, out=torch.full_like(before, math.nan), per_token=per_token, causal=causal, q_start=q_start,
+                               decay=decay, workspace=ws.clone())
+            full = w + decay * before.double()
+            err = (got.double() - full).abs()
+            assert bool((err <= e + 2 * 2.0 ** -24 * (full + decay * before.double()) + 1e-37).all()), (per_token, decay, float(err.max()))
+            old = torch.zeros_like(before) if decay == 0.0 else before * decay
+            gone = ~(held if not per_token else held.repeat_interleave(TILE, -1))
+            assert torch.equal(got[gone], old[gone])
+        mine = before.clone()
+        assert hb.attn_mass(sh, Q, lse, kv, mass=mine, per_token=per_token, causal=causal, q_start=q_start, decay=0.75) is mine
+        assert torch.equal(mine, got)
