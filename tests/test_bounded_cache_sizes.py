@@ -115,3 +115,49 @@ def test_mass_where_held_tiles_are_numbered(B, Hkv, G, T, Lq, causal, ranges, dt
         mine = before.clone()
         assert hb.attn_mass(sh, Q, lse, kv, mass=mine, per_token=per_token, causal=causal, q_start=q_start, decay=0.75) is mine
         assert torch.equal(mine, got)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# choice of tokens: rows in parts of every length
+# ---------------------------------------------------------------------------------------------------------------------
+def _kept(w, keep, first, last):
+    """Tokens of one row that are kept, ascending (numpy, no NaN; the lower token first among equals)."""
+    n = len(w)
+    if n <= keep:
+        return np.arange(n)
+    rest = first + np.argsort(-w[first:n - last], kind="stable")[:keep - first - last]
+    return np.concatenate([np.arange(first), np.sort(rest), np.arange(n - last, n)])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["spread", "alike", "one bin"])
+@pytest.mark.parametrize("B,Hkv,n,ragged", [
+    (1, 1, 400000, False),     # 64 parts of 6400 tokens
+    (5, 4, 70003, True),       # 51 parts of 1536
+    (2, 9, 9001, True),        # 9 parts of 1024
+    (8, 8, 131071, False),     # 16 parts of 8192
+    (8, 8, 262144, True),      # 16 parts of 16384: the most that a part counts, and its keys are read again in every pass
+    (2, 2, 262145, False),     # 64 parts of 4352
+])
+def test_keep_tokens_in_parts_of_every_length(B, Hkv, n, ragged, kind):
+    sh = hb.make_shape(B, Hkv, Hkv, TILE)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    K = torch.randn((1, 1, n, D), generator=g, device="cuda").bfloat16().expand(B, Hkv, n, D)      # heads share their vectors
+    x = torch.rand((B, Hkv, n), generator=g, device="cuda")
+    w = {"spread": torch.exp(3.0 * x - 9.0), "alike": torch.full_like(x, 0.25), "one bin": 1.0 + x / 8}[kind]
+    lens = [n - 7919 * b if b % 3 else n for b in range(B)] if ragged else [n] * B
+    lens = [max(1, m) for m in lens]
+    wn = w.cpu().numpy()
+    for keep, first, last in ((n // 16, 4, 32), (n - n // 3, 0, 1)):
+        ko, vo, index = hb.keep_tokens(sh, K, K, w, keep, first=first, last=last, lens=torch.tensor(lens, dtype=torch.int32, device="cuda") if ragged else None)
+        got = index.cpu().numpy()
+        for b in range(B):
+            for h in range(Hkv):
+                t = _kept(wn[b, h, :lens[b]], keep, first, last)
+                assert (got[b, h, :len(t)] == t).all() and (got[b, h, len(t):] == -1).all(), (keep, b, h)
+        for b, h in ((0, 0), (B - 1, Hkv - 1)):
+            i = index[b, h].long()
+            there = (i >= 0)[:, None]
+            want = torch.where(there, _bits(K[b, h])[i.clamp(min=0)], 0)
+            assert torch.equal(_bits(ko[b, h]), want) and torch.equal(_bits(vo[b, h]), want)
+        del ko, vo, index
