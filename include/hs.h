@@ -408,7 +408,8 @@ HS_API int hs_rope_plan(const hs_rope_params* params, hs_rope* rope);
  * (hs_view strides: any order of the axes.)  positions: device int32 [B, n], or NULL: token i stands at first_position + i in every row.
  * rows: device int32 [B], or NULL: token i of batch row b goes to row rows[b] + i (first_row + i) of k_out and v_out; rows outside
  * 0 .. n_rows - 1 are not written (a sequence that takes no part: rows[b] = -n or below).  Only B, Hq, Hkv, D and dtype of `shape` are
- * looked at beyond its checks.  An output may be the input's memory vector for vector (in place), or not overlap any input or other output. */
+ * looked at beyond its checks.  B n <= 2^29 - 32 (HS_EUNSUPPORTED beyond).  An output may be the input's memory vector for vector (in
+ * place), or not overlap any input or other output. */
 HS_API int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, const int32_t* positions, int32_t first_position,
                 const hs_view* q, const hs_view* q_out, const hs_view* k, const hs_view* k_out, const hs_view* v,
                 const hs_view* v_out, const int32_t* rows, int32_t first_row, int32_t n_rows, void* stream);

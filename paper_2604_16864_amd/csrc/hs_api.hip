@@ -643,7 +643,7 @@ int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, const int
     return HS_EINVAL;
   if (n < 1 || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr)) return HS_EINVAL;
   if ((q == nullptr && k == nullptr) || (v != nullptr && k == nullptr)) return HS_EINVAL;
-  if ((int64_t)shape->B * n > INT32_MAX) return HS_EUNSUPPORTED;
+  if ((int64_t)shape->B * n > (int64_t)HS_MAX_BLOCKS << HS_ROPE_MOST_LOG2) return HS_EUNSUPPORTED;
   if (k != nullptr && n_rows < 1) return HS_EINVAL;
   hs_rope_args a = {};
   a.rope = *rope;

@@ -221,12 +221,16 @@ static inline hs_vec_view hs_make_view(const hs_view* v) {
   if (v == nullptr) return hs_vec_view{nullptr, 0, 0, 0};
   return hs_vec_view{(uint16_t*)v->data, v->batch, v->head, v->token};
 }
+// Workgroups of 256 threads along an axis of a grid.  A launch counts the axis's threads in 32 bits and takes the rest of a larger number without an error.
+enum { HS_MAX_BLOCKS = (1 << 24) - 1 };
 struct hs_rope_args {
   hs_rope rope;
   hs_vec_view q, qo, k, ko, v, vo;
   const int32_t *positions, *rows;
   int32_t n, first_position, first_row, n_rows, B, Hq, Hkv;
 };
+enum { HS_ROPE_MOST_LOG2 = 5 };  // a workgroup takes at most 32 tokens
+// B n <= HS_MAX_BLOCKS << HS_ROPE_MOST_LOG2
 hipError_t hs_launch_rope(const hs_rope_args& a, int dtype, hipStream_t st);
 struct hs_mass_args {
   const uint16_t* q; int64_t q_sb, q_sh, q_st;

@@ -142,7 +142,8 @@ hipError_t hs_launch_rope(const hs_rope_args& a, int dtype, hipStream_t st) {
   // 4096 (101 MB) 22.3 / 27.2, 512 6.55 / 6.5.  (805 MB in 159 us are 5.05 TB/s, what a plain copy of 2 GiB reaches on the card, 4.98.)
   const bool past = at * heads * (2 * HS_D * 2) > (int64_t)256 << 20;
   int lg = 0;
-  while (lg < (past ? 2 : 5) && (2 << lg) <= at) lg++;
+  while (lg < (past ? 2 : HS_ROPE_MOST_LOG2) && (2 << lg) <= at) lg++;
+  while ((at + (1 << lg) - 1) >> lg > HS_MAX_BLOCKS) lg++;  // from 2^26 tokens on; the caller has checked that 32 a workgroup do
   const int64_t blocks = (at + (1 << lg) - 1) >> lg;
   const int step = 32 >> lg;
   int per = (heads + step - 1) / step;

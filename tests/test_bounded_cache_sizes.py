@@ -1,5 +1,6 @@
 """The operators around a bounded cache at the sizes where another kernel or another share of the work is chosen: held tiles numbered by the workgroups
 (attention mass), rows in parts of every length (choice of tokens), counts near what a launch holds.  Plain forms in 64 bits on the device."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -161,3 +162,32 @@ def test_keep_tokens_in_parts_of_every_length(B, Hkv, n, ragged, kind):
             want = torch.where(there, _bits(K[b, h])[i.clamp(min=0)], 0)
             assert torch.equal(_bits(ko[b, h]), want) and torch.equal(_bits(vo[b, h]), want)
         del ko, vo, index
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# counts near what a launch holds
+# ---------------------------------------------------------------------------------------------------------------------
+@gpu
+def test_rope_of_more_tokens_than_four_a_workgroup_hold():
+    """2^26 tokens and more (17 GB of queries of one head): a grid of 4 tokens a workgroup would have 2^32 threads.  All tokens are the same vector."""
+    n = (1 << 26) + 1005
+    sh, rope = hb.make_shape(1, 1, 1, TILE), hb.make_rope()
+    x = torch.randn((1, 1, 1, D), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").bfloat16()
+    out = torch.empty((1, 1, n, D), dtype=torch.bfloat16, device="cuda")
+    hb.rope_qkv(sh, rope, q=x.expand(1, n, 1, D), positions=-9, q_out=out)
+    for first in (0, (1 << 25) - 1000, (1 << 26) - 1000, n - 2000):
+        part, _, _ = hb.rope_qkv(sh, rope, q=x.expand(1, 2000, 1, D), positions=first - 9)
+        assert torch.equal(_bits(out[:, :, first:first + 2000]), _bits(part)), first
+
+
+def _one(token=D):
+    return C.byref(hb.HsView(4096, 0, D, token))
+
+
+def test_rope_refuses_more_tokens_than_a_launch_holds():
+    """(Addresses here are never read.)"""
+    rope = hb.make_rope()
+    for B, n in ((1, (1 << 29) - 31), (2, 1 << 28), (1, 2 ** 31 - 1)):
+        sh = hb.make_shape(B, 1, 1, TILE)
+        out = C.byref(hb.HsView(4096, D, D, D))
+        assert hb.lib().hs_rope_qkv(C.byref(sh), C.byref(rope), n, None, 0, _one(0), out, None, None, None, None, None, 0, 0, None) == -2, (B, n)
