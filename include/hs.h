@@ -458,7 +458,7 @@ HS_API int hs_evict_tiles(const hs_shape* shape, const hs_kv* kv, const float* m
  *   weight    device fp32, element strides weight_strides[2] = {batch, head} (NULL: contiguous [B, Hkv, n_tokens]), tokens contiguous
  *   index     device int32 [B, Hkv, keep]: the tokens kept
  * A row of fewer than `keep` tokens keeps them all; the rest of its outputs is 0 and its indices -1.  keep >= first + last,
- * 1 <= keep <= 2^30, n_tokens <= 2^20.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  Outputs overlap neither
+ * 1 <= keep <= 2^28 - 16, n_tokens <= 2^20.  Only B, Hq, Hkv, D and dtype of `shape` are looked at beyond its checks.  Outputs overlap neither
  * inputs nor each other.  workspace: hs_workspace_bytes(op 5, n_tokens), 16-byte aligned (NULL where that is 0), not shared between
  * two calls in flight; no initial content. */
 HS_API int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, const hs_view* V, const float* weight,

@@ -743,7 +743,7 @@ int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, co
   int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (n_tokens < 1 || K == nullptr || V == nullptr || weight == nullptr || K_out == nullptr || V_out == nullptr || index == nullptr) return HS_EINVAL;
-  if (n_tokens > 1 << 20 || keep > 1 << 30) return HS_EUNSUPPORTED;
+  if (n_tokens > 1 << 20 || keep > HS_KEEP_GATHERED * HS_MAX_BLOCKS) return HS_EUNSUPPORTED;
   if ((((uintptr_t)K_out | (uintptr_t)V_out) & 15u) || (((uintptr_t)weight | (uintptr_t)index) & 3u)) return HS_EINVAL;
   if (keep < 1 || first < 0 || last < 0 || (int64_t)first + last > keep) return HS_EINVAL;
   if (((uintptr_t)workspace & 15u) || (workspace == nullptr && hs_keep_ws_bytes((int64_t)shape->B * shape->Hkv, n_tokens) != 0)) return HS_EINVAL;

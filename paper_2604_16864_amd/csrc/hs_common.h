@@ -251,6 +251,7 @@ static inline size_t hs_evict_ws_ints(int64_t rows, int T) { return (size_t)rows
 hipError_t hs_launch_evict(int B, int Hkv, int T, const hs_kv_dev& kv, const float* mass, int keep, const int32_t* keeps, int first, int last,
                            int32_t* ws, hipStream_t st);
 enum { HS_KEEP_SHORT = 4096 };  // tokens of a row up to which one workgroup ranks them, without a workspace
+enum { HS_KEEP_GATHERED = 16 };  // output rows of a workgroup that gathers: keep <= HS_KEEP_GATHERED * HS_MAX_BLOCKS
 size_t hs_keep_ws_bytes(int64_t rows, int n);
 hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
                           int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, void* ws, hipStream_t st);

@@ -466,7 +466,7 @@ __global__ __launch_bounds__(256) void keep_take_kernel(KeepArgs A, KeepWs ws) {
 __global__ __launch_bounds__(256) void keep_gather_kernel(int Hkv, int keep, hs_vec_view K, hs_vec_view V, const int32_t* __restrict__ index, uint16_t* __restrict__ K_out,
                                                           uint16_t* __restrict__ V_out) {
   const int row = blockIdx.y, b = row / Hkv, h = row % Hkv, c = threadIdx.x & 15;
-  const int i = blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int i = blockIdx.x * HS_KEEP_GATHERED + (threadIdx.x >> 4);
   if (i >= keep) return;
   const int64_t at = (int64_t)row * keep + i;
   const int t = index[at];
@@ -514,6 +514,6 @@ hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, c
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(keep_gather_kernel, dim3((keep + 15) / 16, rows), dim3(256), 0, st, Hkv, keep, K, V, index, K_out, V_out);
+  hipLaunchKernelGGL(keep_gather_kernel, dim3((keep + HS_KEEP_GATHERED - 1) / HS_KEEP_GATHERED, rows), dim3(256), 0, st, Hkv, keep, K, V, index, K_out, V_out);
   return hipGetLastError();
 }

@@ -191,3 +191,11 @@ def test_rope_refuses_more_tokens_than_a_launch_holds():
         sh = hb.make_shape(B, 1, 1, TILE)
         out = C.byref(hb.HsView(4096, D, D, D))
         assert hb.lib().hs_rope_qkv(C.byref(sh), C.byref(rope), n, None, 0, _one(0), out, None, None, None, None, None, 0, 0, None) == -2, (B, n)
+
+
+def test_keep_tokens_refuses_more_rows_than_a_launch_holds():
+    """(Addresses here are never read.)"""
+    sh = hb.make_shape(1, 2, 2, TILE)
+    K = C.byref(hb.HsView(4096, 0, 100 * D, D))
+    for keep in ((1 << 28) - 15, 1 << 28, 1 << 30):
+        assert hb.lib().hs_keep_tokens(C.byref(sh), 100, K, K, 4096, None, None, keep, 0, 0, 4096, 4096, 4096, 4096, None) == -2, keep
