@@ -421,7 +421,8 @@ HS_API int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, co
  * A query whose LSE is not finite (one that saw nothing; one the caller leaves out by setting its LSE to -inf) weighs nothing.
  *   Q     [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i and sees what hs_prefill_attn_at lets it see (0 <= q_start,
  *         q_start + Lq <= L if causal, else q_start is not looked at)
- *         (HS_EUNSUPPORTED where the queries and LSEs of 32 positions of a group's heads lie further than 4 GiB apart)
+ *         (HS_EUNSUPPORTED where the queries and LSEs of 32 positions of a group's heads lie further than 4 GiB apart, where the Hkv
+ *         rows of a batch row have more than 2^31 - 1 tiles, and, but for one query that is not causal, where Hkv ceil(L / 256) reaches 2^24)
  *   LSE   fp32, element strides lse_strides[2] = {batch, head} (NULL: contiguous [B, Hq, Lq]), queries contiguous
  *   mass  fp32 [B, Hkv, L / 64], or with per_token [B, Hkv, L]; mass_in NULL: zeros (as with decay 0, when it is not read); mass_out may be
  *         mass_in.  Tiles that are SKIP get decay mass_in.

@@ -707,7 +707,10 @@ int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale
   if ((double)q.st * 62.0 + (double)q.sh * 14.0 >= 4294967040.0 || (double)l_sh * 28.0 >= 4294967040.0) return HS_EUNSUPPORTED;
   hs_mass_args a = {};
   a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, causal != 0, per_token != 0);
-  if ((int64_t)a.n_ranges * shape->Hkv * (shape->L / HS_BT) > INT32_MAX) return HS_EUNSUPPORTED;  // the grid
+  if ((int64_t)a.n_ranges * shape->Hkv * (shape->L / HS_BT) > INT32_MAX) return HS_EUNSUPPORTED;
+  // the grid of the kernel for many queries
+  if ((Lq > 1 || causal) && (int64_t)a.n_ranges * shape->Hkv * ((shape->L / HS_BT + HS_MASS_TILES - 1) / HS_MASS_TILES) > HS_MAX_BLOCKS)
+    return HS_EUNSUPPORTED;
   if (a.n_ranges > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
   a.q = q.p; a.q_sb = q.sb; a.q_sh = q.sh; a.q_st = q.st;
   a.lse = LSE;

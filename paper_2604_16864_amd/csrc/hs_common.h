@@ -243,6 +243,7 @@ struct hs_mass_args {
   int32_t B, Hq, Hkv, T, Lq, q_start, causal, tail_len, tail_tile, per_token, n_ranges, numbered;
   float scale, decay;
 };
+enum { HS_MASS_TILES = 4 };  // tiles of a workgroup: n_ranges * Hkv * ceil(T / HS_MASS_TILES) <= HS_MAX_BLOCKS where Lq > 1 or causal
 // ranges that the queries of a call are cut into; with more than one, ws = n_ranges * B * Hkv * (T or 64 T) floats
 int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_token);
 hipError_t hs_launch_mass(const hs_mass_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);

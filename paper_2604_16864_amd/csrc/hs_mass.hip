@@ -298,7 +298,7 @@ __device__ __forceinline__ void lds_load4(uint32_t base, const void* p, uint32_t
 
 constexpr int kStages = 4;                        // two blocks are worked on while the next two are on their way
 constexpr int kStageBytes = 8 * 1024 + 256;       // 32 columns of 256 bytes, and the columns' LSE (twice)
-constexpr int kGroup = 4;                         // tiles of a workgroup
+constexpr int kGroup = HS_MASS_TILES;
 constexpr int kAhead = 2;                         // pairs of exponentials in front of a block's first products
 // Products of a block beside the exponentials of the one before (two sets of scores), or one set and, for the registers that this frees, 3 waves per
 // SIMD instead of 2 (dense keys).  us, beside / one set: dense keys per tile, 4096 queries on 16K tokens 470 / 460, 512 on 4 x 4K 85 / 81, a 2K prompt

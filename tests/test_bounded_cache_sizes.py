@@ -199,3 +199,12 @@ def test_keep_tokens_refuses_more_rows_than_a_launch_holds():
     K = C.byref(hb.HsView(4096, 0, 100 * D, D))
     for keep in ((1 << 28) - 15, 1 << 28, 1 << 30):
         assert hb.lib().hs_keep_tokens(C.byref(sh), 100, K, K, 4096, None, None, keep, 0, 0, 4096, 4096, 4096, 4096, None) == -2, keep
+
+
+def test_mass_refuses_more_tiles_than_a_launch_holds():
+    """Caches of positions for 2^26 tiles in a batch row's kv heads, nearly all of them missing.  (Addresses here are never read.)"""
+    kv = C.byref(hb.HsKV(k_map=4096, v_map=4096))
+    for Hkv, L, Lq, causal in ((8, 1 << 29, 8, 1), (64, 1 << 26, 1, 1), (3, 2 ** 31 - 64, 200, 0)):
+        sh = hb.make_shape(1, Hkv, Hkv, L)
+        Q = C.byref(hb.HsView(4096, 0, 1024 * D, D))
+        assert hb.lib().hs_attn_mass(C.byref(sh), Lq, 0, 0.0, causal, Q, 4096, None, kv, None, 0, None, 0, None, 0, 1.0, None, 4096, 4096, None) == -2, (Hkv, L)
