@@ -602,11 +602,19 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_STRETCH, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 OP_EVICT, OP_KEEP = 4, 5      # hs_workspace_bytes: scratch of evict_tiles, and of keep_tokens (arg: tokens)
 
 
+def _i32(x):
+    """A number that the library takes as int32: others are refused here (ctypes would keep their lower 32 bits)."""
+    x = int(x)
+    if not -1 << 31 <= x < 1 << 31:
+        raise HsError(f"{x} is not a 32-bit integer")
+    return x
+
+
 def make_rope(rot_dim=HEAD_DIM, layout=ROPE_HALVES, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, low=0.0, high=0.0, trained=0):
     """The angles of rope_qkv (hs_rope_plan): rot_dim channels of a head turn (a multiple of 16), channel i with i + rot_dim / 2 (ROPE_HALVES) or
     2i with 2i + 1 (ROPE_PAIRS).  scaling stretches the context by `factor`: ROPE_LINEAR, ROPE_STRETCH (of the base), ROPE_BANDS and ROPE_RAMP
     (by the turns a pair makes over the `trained` tokens: more than `high` keep their angle, fewer than `low` are divided)."""
-    params = HsRopeParams(int(rot_dim), int(layout), int(scaling), int(trained), float(base), float(factor), float(low), float(high))
+    params = HsRopeParams(_i32(rot_dim), _i32(layout), _i32(scaling), _i32(trained), float(base), float(factor), float(low), float(high))
     rope = HsRope()
     _check(lib().hs_rope_plan(C.byref(params), C.byref(rope)))
     return rope
@@ -640,8 +648,9 @@ def rope_qkv(shape, rope, q=None, k=None, v=None, positions=0, q_out=None, k_out
         return _done(r)
     some = q if q is not None else k
     assert some is not None and (v is None or k is not None)
+    B, n = some.shape[0], _i32(some.shape[1])
+    first, row0 = (0 if torch.is_tensor(x) else _i32(x) for x in (positions, rows))
     _here(q, k, v, q_out, k_out, v_out)
-    B, n = some.shape[0], some.shape[1]
     for t, heads in ((q, shape.Hq), (k, shape.Hkv), (v, shape.Hkv)):
         assert t is None or (t.dtype == torch_dtype(shape) and tuple(t.shape) == (shape.B, n, heads, shape.D))
     if q is not None and q_out is None:
@@ -652,12 +661,12 @@ def rope_qkv(shape, rope, q=None, k=None, v=None, positions=0, q_out=None, k_out
         v_out = v.new_empty(k_out.shape)
     assert (q is not None or q_out is None) and (k is not None or k_out is None) and (v is not None or v_out is None)
     assert q_out is None or (q_out.dtype == q.dtype and tuple(q_out.shape) == (B, shape.Hq, n, shape.D))
-    n_rows = 0 if k_out is None else k_out.shape[2]
+    n_rows = 0 if k_out is None else _i32(k_out.shape[2])
     for t in (k_out, v_out):
         assert t is None or (t.dtype == k.dtype and tuple(t.shape) == (B, shape.Hkv, n_rows, shape.D))
     views = [None if t is None else _view(t, h, i) for t, h, i in ((q, 2, 1), (q_out, 1, 2), (k, 2, 1), (k_out, 1, 2), (v, 2, 1), (v_out, 1, 2))]
-    pos, first = (_int32(positions, (B, n)), 0) if torch.is_tensor(positions) else (None, int(positions))
-    at, row0 = (_int32(rows, (B,)), 0) if torch.is_tensor(rows) else (None, int(rows))
+    pos = _int32(positions, (B, n)) if torch.is_tensor(positions) else None
+    at = _int32(rows, (B,)) if torch.is_tensor(rows) else None
     _here(*(t for t in (positions, rows) if torch.is_tensor(t)))
     _check(lib().hs_rope_qkv(C.byref(shape), C.byref(rope), n, pos, first, *(None if x is None else C.byref(x) for x in views), at, row0,
                              n_rows, _stream()))
@@ -679,8 +688,10 @@ def attn_mass(shape, Q, lse, kv, mass=None, out=None, per_token=False, decay=1.0
         causal = Q.dim() == 4
     if Q.dim() == 3:
         Q, lse = Q.unsqueeze(2), lse.unsqueeze(2)
+    Lq, T = _i32(Q.shape[2]), shape.L // TILE
+    at = _i32(shape.L - Lq if q_start is None else q_start) if causal else 0
+    n_tail, n_tile = (0 if tail_k is None or x is None or torch.is_tensor(x) else _i32(x) for x in (tail_len, tail_tile))
     _here(Q, lse, mass, out, tail_k, workspace, kv.k_map)
-    Lq, T = Q.shape[2], shape.L // TILE
     assert Q.dtype == torch_dtype(shape) and tuple(Q.shape) == (shape.B, shape.Hq, Lq, shape.D)
     assert lse.dtype == torch.float32 and tuple(lse.shape) == (shape.B, shape.Hq, Lq) and (Lq == 1 or lse.stride(2) == 1)
     sizes = (shape.B, shape.Hkv, shape.L if per_token else T)
@@ -688,21 +699,19 @@ def attn_mass(shape, Q, lse, kv, mass=None, out=None, per_token=False, decay=1.0
         out = Q.new_empty(sizes, dtype=torch.float32) if mass is None else mass
     for t in (mass, out):
         assert t is None or (t.dtype == torch.float32 and tuple(t.shape) == sizes and t.is_contiguous())
-    n_tail, lens, n_tile, tiles = 0, None, 0, None
+    lens, tiles = None, None
     if tail_k is not None:
         assert tail_len is not None and tail_tile is not None
         assert tail_k.dtype == Q.dtype and tail_k.is_contiguous() and tuple(tail_k.shape) == (shape.B, shape.Hkv, TILE, shape.D)
-        n_tail, lens = (0, _int32(tail_len, (shape.B,))) if torch.is_tensor(tail_len) else (int(tail_len), None)
-        n_tile, tiles = (0, _int32(tail_tile, (shape.B,))) if torch.is_tensor(tail_tile) else (int(tail_tile), None)
+        lens, tiles = (_int32(x, (shape.B,)) if torch.is_tensor(x) else None for x in (tail_len, tail_tile))
         _here(*(t for t in (tail_len, tail_tile) if torch.is_tensor(t)))
     need = C.c_size_t(0)
     _check(lib().hs_attn_mass_workspace_bytes(C.byref(shape), Lq, int(bool(causal)), int(bool(per_token)), C.byref(need)))
     if workspace is None:
         workspace = _workspace(need.value, Q.device) if need.value else None
     assert workspace is None or workspace.nbytes >= need.value
-    at = shape.L - Lq if q_start is None else int(q_start)
     kvs = kv.struct()
-    _check(lib().hs_attn_mass(C.byref(shape), Lq, at if causal else 0, float(scale), int(bool(causal)), C.byref(_view(Q, 1, 2)), _ptr(lse),
+    _check(lib().hs_attn_mass(C.byref(shape), Lq, at, float(scale), int(bool(causal)), C.byref(_view(Q, 1, 2)), _ptr(lse),
                               (C.c_int64 * 2)(lse.stride(0), lse.stride(1)), C.byref(kvs), _ptr(tail_k), n_tail, lens, n_tile, tiles,
                               int(bool(per_token)), float(decay), _ptr(mass), _ptr(out), _ptr(workspace), _stream()))
     return out
@@ -711,7 +720,7 @@ def attn_mass(shape, Q, lse, kv, mass=None, out=None, per_token=False, decay=1.0
 def attn_mass_workspace_bytes(shape, Lq, causal=True, per_token=False):
     """Scratch that attn_mass takes for this call."""
     need = C.c_size_t(0)
-    _check(lib().hs_attn_mass_workspace_bytes(C.byref(shape), int(Lq), int(bool(causal)), int(bool(per_token)), C.byref(need)))
+    _check(lib().hs_attn_mass_workspace_bytes(C.byref(shape), _i32(Lq), int(bool(causal)), int(bool(per_token)), C.byref(need)))
     return need.value
 
 
@@ -722,9 +731,10 @@ def evict_tiles(shape, kv, mass, keep, first=0, last=0, workspace=None):
     if _done(_fast().evict(shape, kv, mass, keep, first, last, workspace)) is not None:
         kv.uniform = 0
         return
+    n, first, last = 0 if torch.is_tensor(keep) else _i32(keep), _i32(first), _i32(last)
     _here(mass, workspace, kv.k_map)
     assert mass.dtype == torch.float32 and mass.is_contiguous() and tuple(mass.shape) == (shape.B, shape.Hkv, shape.L // TILE)
-    n, per_row = (0, _int32(keep, (shape.B, shape.Hkv))) if torch.is_tensor(keep) else (int(keep), None)
+    per_row = _int32(keep, (shape.B, shape.Hkv)) if torch.is_tensor(keep) else None
     if torch.is_tensor(keep):
         _here(keep)
     need = workspace_bytes(shape, OP_EVICT)
@@ -733,7 +743,7 @@ def evict_tiles(shape, kv, mass, keep, first=0, last=0, workspace=None):
     assert workspace.nbytes >= need
     kvs = kv.struct()
     kvs.uniform = 0
-    _check(lib().hs_evict_tiles(C.byref(shape), C.byref(kvs), _ptr(mass), n, per_row, int(first), int(last), _ptr(workspace), _stream()))
+    _check(lib().hs_evict_tiles(C.byref(shape), C.byref(kvs), _ptr(mass), n, per_row, first, last, _ptr(workspace), _stream()))
     kv.uniform = 0
 
 
@@ -745,8 +755,8 @@ def keep_tokens(shape, K, V, weight, keep, first=0, last=0, lens=None):
     r = _fast().keep(shape, K, V, weight, keep, first, last, lens)
     if r is not None:
         return _done(r)
+    n, keep, first, last = _i32(K.shape[2]), _i32(keep), _i32(first), _i32(last)
     _here(K, V, weight, lens)
-    n, keep = K.shape[2], int(keep)
     assert K.dtype == torch_dtype(shape) and V.dtype == K.dtype and K.shape == V.shape and tuple(K.shape) == (shape.B, shape.Hkv, n, shape.D)
     assert weight.dtype == torch.float32 and tuple(weight.shape) == (shape.B, shape.Hkv, n) and (n == 1 or weight.stride(2) == 1)
     at = None if lens is None else _int32(lens, (shape.B,))
@@ -757,7 +767,7 @@ def keep_tokens(shape, K, V, weight, keep, first=0, last=0, lens=None):
     need = workspace_bytes(shape, OP_KEEP, n)
     workspace = _workspace(need, K.device) if need else None
     _check(lib().hs_keep_tokens(C.byref(shape), n, C.byref(_view(K, 1, 2)), C.byref(_view(V, 1, 2)), _ptr(weight),
-                                (C.c_int64 * 2)(weight.stride(0), weight.stride(1)), at, keep, int(first), int(last), _ptr(K_out), _ptr(V_out),
+                                (C.c_int64 * 2)(weight.stride(0), weight.stride(1)), at, keep, first, last, _ptr(K_out), _ptr(V_out),
                                 _ptr(index), _ptr(workspace), _stream()))
     return K_out, V_out, index
 

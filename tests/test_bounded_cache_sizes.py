@@ -208,3 +208,21 @@ def test_mass_refuses_more_tiles_than_a_launch_holds():
         sh = hb.make_shape(1, Hkv, Hkv, L)
         Q = C.byref(hb.HsView(4096, 0, 1024 * D, D))
         assert hb.lib().hs_attn_mass(C.byref(sh), Lq, 0, 0.0, causal, Q, 4096, None, kv, None, 0, None, 0, None, 0, 1.0, None, 4096, 4096, None) == -2, (Hkv, L)
+
+
+def test_binding_refuses_numbers_that_are_no_int32():
+    """Numbers whose lower 32 bits would be another call's: refused before the tensors are looked at."""
+    sh, rope = hb.make_shape(1, 4, 2, 128), hb.make_rope()
+    q, k = torch.zeros((1, 3, 4, D), dtype=torch.bfloat16), torch.zeros((1, 3, 2, D), dtype=torch.bfloat16)
+    kv, Q, lse, mass = hb.PackedKV(sh, [0, 0, 2, 0, 2], "cpu"), q.transpose(1, 2), torch.zeros(1, 4, 3), torch.zeros(1, 2, 2)
+    tail, one, one_lse = torch.zeros((1, 2, TILE, D), dtype=torch.bfloat16), torch.zeros((1, 4, D), dtype=torch.bfloat16), torch.zeros(1, 4)
+    K, w = k.transpose(1, 2), torch.zeros(1, 2, 3)
+    for big in ((1 << 32) + 1, 1 << 31, -(1 << 31) - 1):
+        for call in (lambda: hb.make_rope(rot_dim=big), lambda: hb.make_rope(trained=big), lambda: hb.rope_qkv(sh, rope, q, positions=big),
+                     lambda: hb.rope_qkv(sh, rope, None, k, rows=big), lambda: hb.attn_mass(sh, Q, lse, kv, q_start=big),
+                     lambda: hb.attn_mass(sh, one, one_lse, kv, tail_k=tail, tail_len=big, tail_tile=0), lambda: hb.attn_mass(sh, one, one_lse, kv, tail_k=tail, tail_len=1, tail_tile=big),
+                     lambda: hb.attn_mass_workspace_bytes(sh, big), lambda: hb.evict_tiles(sh, kv, mass, big), lambda: hb.evict_tiles(sh, kv, mass, 1, first=big),
+                     lambda: hb.evict_tiles(sh, kv, mass, 1, last=big), lambda: hb.keep_tokens(sh, K, K, w, big), lambda: hb.keep_tokens(sh, K, K, w, 2, first=big),
+                     lambda: hb.keep_tokens(sh, K, K, w, 2, last=big), lambda: hb.rope_qkv(sh, rope, q[:, :1].expand(1, (1 << 31) + 5, 4, D))):
+            with pytest.raises(hb.HsError, match="32-bit"):
+                call()
