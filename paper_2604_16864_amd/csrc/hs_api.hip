@@ -669,12 +669,13 @@ int hs_rope_qkv(const hs_shape* shape, const hs_rope* rope, int32_t n, const int
 }
 
 int hs_attn_mass_workspace_bytes(const hs_shape* shape, int32_t Lq, int causal, int per_token, size_t* bytes) {
+  (void)causal;  // so far the same either way
   const int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (Lq < 1 || bytes == nullptr) return HS_EINVAL;
   if (Lq > 1 << 30) return HS_EUNSUPPORTED;
   const int T = shape->L / HS_BT;
-  const int n = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, T, Lq, causal != 0, per_token != 0);
+  const int n = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, T, Lq, per_token != 0);
   *bytes = n > 1 ? (size_t)n * shape->B * shape->Hkv * T * (per_token != 0 ? HS_BT : 1) * sizeof(float) : 0;
   return HS_OK;
 }
@@ -706,7 +707,7 @@ int hs_attn_mass(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale
   // the kernel for many queries reads the queries of 32 / G positions and G heads by 32-bit byte offsets
   if ((double)q.st * 62.0 + (double)q.sh * 14.0 >= 4294967040.0 || (double)l_sh * 28.0 >= 4294967040.0) return HS_EUNSUPPORTED;
   hs_mass_args a = {};
-  a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, causal != 0, per_token != 0);
+  a.n_ranges = hs_mass_ranges(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, per_token != 0);
   if ((int64_t)a.n_ranges * shape->Hkv * (shape->L / HS_BT) > INT32_MAX) return HS_EUNSUPPORTED;
   // the grid of the kernel for many queries
   if ((Lq > 1 || causal) && (int64_t)a.n_ranges * shape->Hkv * ((shape->L / HS_BT + HS_MASS_TILES - 1) / HS_MASS_TILES) > HS_MAX_BLOCKS)

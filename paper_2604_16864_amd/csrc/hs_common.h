@@ -217,10 +217,6 @@ int hs_prefill_auto_splits(int B, int Hq, int Hkv, int T, int Lq, int q_start, i
 
 // -------- rotary positions, attention mass, eviction, token choice --------
 struct hs_vec_view { uint16_t* p; int64_t sb, sh, st; };  // D-channel vectors: element strides of batch, head, token
-static inline hs_vec_view hs_make_view(const hs_view* v) {
-  if (v == nullptr) return hs_vec_view{nullptr, 0, 0, 0};
-  return hs_vec_view{(uint16_t*)v->data, v->batch, v->head, v->token};
-}
 // Workgroups of 256 threads along an axis of a grid.  A launch counts the axis's threads in 32 bits and takes the rest of a larger number without an error.
 enum { HS_MAX_BLOCKS = (1 << 24) - 1 };
 struct hs_rope_args {
@@ -245,7 +241,7 @@ struct hs_mass_args {
 };
 enum { HS_MASS_TILES = 4 };  // tiles of a workgroup: n_ranges * Hkv * ceil(T / HS_MASS_TILES) <= HS_MAX_BLOCKS where Lq > 1 or causal
 // ranges that the queries of a call are cut into; with more than one, ws = n_ranges * B * Hkv * (T or 64 T) floats
-int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_token);
+int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int per_token);
 hipError_t hs_launch_mass(const hs_mass_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);
 // ws: hs_evict_ws_ints ints
 static inline size_t hs_evict_ws_ints(int64_t rows, int T) { return (size_t)rows * (4 + 2 * (size_t)(T + 1)); }

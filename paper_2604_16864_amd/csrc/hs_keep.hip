@@ -22,7 +22,7 @@ __device__ __forceinline__ void count_bins(int* hist, uint32_t key, bool valid) 
 // One workgroup per row.  Weights are read three times, the last two from the L2: a histogram of the keys' upper 11 bits finds the bin that the
 // last token kept falls into; that bin's tokens are listed in LDS and ranked there exactly (radix selection over key and place, so that ties go
 // by place); then every wave writes the tokens kept of its own part of the row, behind those of the parts before it.
-constexpr int kList = 4096;
+constexpr int kList = HS_KEEP_SHORT;
 template <int NT>
 __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const float* __restrict__ weight, int64_t w_sb, int64_t w_sh, const int32_t* __restrict__ lens,
                                                          int keep, int first, int last, int32_t* __restrict__ index) {
@@ -93,11 +93,11 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
     const int rest = want - bin.below;  // of the bin's tokens
     // the wave's tokens that are taken for certain, and the list of the bin's
     int sure = 0;
-    const bool whole = rest == bin.in, listed = bin.in <= kList;
+    const bool whole = rest == bin.in;
     part([&](int t, uint32_t key, bool valid) {
       const int its = (int)(key >> 21);
       sure += __builtin_popcountll(__ballot(valid && (whole ? its <= bin.bin : its < bin.bin)));
-      if (!whole && listed) {
+      if (!whole) {
         const bool mine = valid && its == bin.bin;
         const unsigned long long all = __ballot(mine);
         if (all != 0ull) {
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
     __syncthreads();
     if (whole) {
       bound = (uint64_t)(uint32_t)bin.bin << 53 | (~0ull >> 11);
-    } else if (listed) {
+    } else {
       bound = smallest_bound<NT>(rest, [&](auto fn) {
         for (int i = tid; i < bin.in; i += NT) fn(list[i]);
       }, &rank);
@@ -125,17 +125,6 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
           atomicAdd(&taken[p], 1);
         }
       }
-    } else {  // most weights alike: ranked where they are
-      bound = smallest_bound<NT>(rest, [&](auto fn) {
-        part([&](int t, uint32_t key, bool valid) {
-          if (valid && (int)(key >> 21) == bin.bin) fn(rank_of(key, t));
-        });
-      }, &rank);
-      int more = 0;
-      part([&](int t, uint32_t key, bool valid) {
-        more += __builtin_popcountll(__ballot(valid && (int)(key >> 21) == bin.bin && rank_of(key, t) <= bound));
-      });
-      if (l == 0) taken[w] += more;
     }
     __syncthreads();
   }

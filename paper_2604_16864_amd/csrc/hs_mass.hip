@@ -582,8 +582,7 @@ __global__ __launch_bounds__(256) void mass_join_kernel(hs_mass_args A, int64_t 
 
 }  // namespace
 
-int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int causal, int per_token) {
-  (void)causal;
+int hs_mass_ranges(int B, int Hq, int Hkv, int T, int Lq, int per_token) {
   if (Lq == 1) return 1;
   const int64_t rows = (int64_t)B * Hkv, groups = rows * ((T + kGroup - 1) / kGroup), queries = 32 / (Hq / Hkv), blocks = (Lq + queries - 1) / queries;
   const int64_t out_bytes = rows * T * (per_token ? HS_BT : 1) * 4;
