@@ -136,7 +136,8 @@ typedef struct {
  *   x_meta   [B, Hkv, cap_sparse_x,  1024 B]   2-bit positions
  *   x_map    [B, Hkv, T] int32: +(slot+1) dense, -(slot+1) sparse, 0 skipped;
  *            slots are handed out in ascending tile order per pool (the two
- *            running counters of Sec. III-B).
+ *            running counters of Sec. III-B); hs_evict_tiles moves tiles to freed
+ *            slots, in any order.  The used slots of a pool are 0 .. n - 1.
  * Inside a tile slot the bytes are in the order in which the lanes of the gfx950
  * matrix instructions consume them (64 lanes x 16 B per chunk; the exact index
  * formulas are in csrc/hs_common.h); hs_unpack_kv returns the logical content.

@@ -124,6 +124,8 @@ static inline hs_kv_dev hs_make_kv_dev(const hs_kv* kv) {
 // tensors, and in one of them shared out between dense and 2:4 = nothing is skipped (so does `uniform`).  Anything else --
 // room beyond a slot per tile, as for states that come as device memory, or one pool of a slot per tile without the promise, as
 // for a cache that grows -- says nothing: any part of a row may be skipped, and rows may differ.
+// hs_evict_tiles leaves the pools' sizes as they are, so a mixed cache that has lost tiles may still count as one that skips nothing.
+// What is chosen by the answer is how a call is shared out; no result depends on it.
 enum hs_kept { HS_KEPT_ALL, HS_KEPT_FEWER, HS_KEPT_UNKNOWN };
 static inline hs_kept hs_kept_by_pools(const hs_kv_dev& kv, int T) {
   const int64_t k = (int64_t)kv.cap_dense_k + kv.cap_sparse_k, v = (int64_t)kv.cap_dense_v + kv.cap_sparse_v;

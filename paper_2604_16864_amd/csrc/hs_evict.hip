@@ -36,8 +36,8 @@ __device__ __forceinline__ void copy_tile(const hs_kv_dev& kv, int64_t row, int 
 }
 
 // One workgroup per row.  A thread holds PER tiles in registers (PER > 0, T <= NT PER), or walks the row's maps (PER == 0).
-// Latency-bound: a chain of a map read, prefix counts, a radix selection and the slots' bookkeeping, about 20 barriers (128 rows of 1024
-// tiles, one too many in each: 8.3 us, 1.7 of them the copies; 32 rows of 1024 tiles down to 256: 9.7, 2.8 of them the selection).
+// Latency-bound: a chain of a map read, prefix counts, the choice and the slots' bookkeeping, 9 barriers where one tile goes (128 rows of 1024
+// tiles: 8.3 us, 1.7 of them the copies), 15 to 20 with a radix selection (32 rows of 1024 tiles down to 256: 9.7, 2.8 of them the selection).
 // COPY: the row's moves are made here, too (few, by the host's count); otherwise they are listed for evict_move_kernel.
 template <int NT, int PER, bool COPY>
 __global__ __launch_bounds__(NT) void evict_kernel(int T, hs_kv_dev kv, const float* __restrict__ mass, int keep, const int32_t* __restrict__ keeps,

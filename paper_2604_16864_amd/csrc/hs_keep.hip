@@ -146,10 +146,14 @@ __global__ __launch_bounds__(NT) void keep_select_kernel(int Hkv, int n, const f
 // ---- long rows ----
 // A workgroup takes a part of a row's candidates, and what one has found the others read in the next launch: (1) a histogram per part of the
 // keys' upper 11 bits; (2) every part adds the row's up, finds the bin that the last token kept falls into, and lists its own
-// tokens of that bin; (3) every part ranks the row's list (the same in each, a few hundred tokens as a rule), and writes the indices of its
-// own tokens kept behind those of the parts before it.  At most 64 parts: what they have found is a lane each.  One workgroup a row spends 27 us per
-// 32K tokens on its arithmetic alone.
-// Latency-bound, three launches: 8 rows of 32K tokens 3.6 + 4.8 + 6.5 us, 32 rows of up to 128K 6.4 + 7.3 + 12.0.
+// tokens of that bin; (3) every part ranks the row's list (the same in each), and writes the indices of its own tokens kept behind those
+// of the parts before it.  At most 64 parts: what they have found is a lane each.  One workgroup a row spends 27 us per 32K tokens on its
+// arithmetic alone.
+// Latency-bound, three launches: 8 rows of 32K tokens 3.6 + 4.8 + 6.5 us, 32 rows of up to 128K 6.4 + 7.3 + 12.0, for weights whose logarithm has a spread
+// of 2: their bin, a quarter of a power of two, holds about a thousand of 128K.  The narrower the weights, the more it holds, and lists beyond
+// kLdsList are read from the L2 in every pass, bins beyond kLongList (unless their keys are all alike) leave every part to rank the whole row by loads that
+// wait for each other.  us of the whole call, 32 rows of 128K tokens, 8192 / 32768 kept: spread 2 69 / 239, 1 74 / 254, 0.5 95 /
+// 1045, 0.1 942 / 1151, uniform in 0 .. 1 883 / 1055, one bin 1020 / 1098, all alike 71 / 211; 8 rows of 32K, 4096 kept: 20.9, 22.3, 28.7, 34.8, 30.6, 128, 19.8.
 constexpr int kParts = 64, kLongList = 8192, kLdsList = 2048;
 constexpr int kCoarse = 64, kFine = kBins / kCoarse;  // a histogram's bins, also in sums of 32
 struct KeepRow {            // per row, in the workspace

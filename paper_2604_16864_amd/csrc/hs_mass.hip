@@ -154,10 +154,12 @@ __global__ __launch_bounds__(256) void mass_step_kernel(hs_mass_args A, hs_kv_de
 }
 
 // ---- many queries ----
-// What bounds it: per score one fused multiply-add, one exponential (two issue slots) and one addition of the vector ALU, 77 % of whose time
-// they take (32 columns and a tile: 814 clocks, of which 552 are these and the issue of 10 matrix instructions; the matrix pipe is 39 %
-// busy), at 2.1 GHz, which the power limit holds: a 16K prompt, 32 heads, 2:4 keys 800 us; 4096 queries on 16K tokens, 2:4 keys per tile 366, per
-// token 396, dense keys 460 and 481.  A barrier every two blocks, and the columns' LSE once, are worth 1 to 2 % of it.  Measured beside it: two tiles a wave, for half
+// What bounds it: the vector ALU.  Per score it has a fused multiply-add, an exponential (two issue slots) and an addition.  In a 16K prompt, 32
+// heads, 2:4 keys, 32 columns and a tile take 807 clocks of a SIMD; in 627 of them (78 %, by the counters) it issues 125 instructions and the 32
+// exponentials' second slots, 4 clocks each: 552 are the scores' three instructions and 10 matrix ones, the rest addresses, limits and the blocks in
+// which a query's view ends.  The matrix pipe is busy for 40 %.  The power limit holds the clock at 2.0 to 2.1 GHz.
+// us, on one card: the prompt 813, per token 863; 4096 queries on 16K tokens, 2:4 keys per tile 369, per token 400, dense keys 478 and 500.  A barrier
+// every two blocks, and the columns' LSE once, are worth 1 to 2 % of it.  Measured beside it, where the prompt took 800: two tiles a wave, for half
 // of the reads of LDS and L2, 1005 (2 waves per SIMD instead of 3); the scheduler's own order, products first, 1155.
 //
 // The queries of a kv head's group pass by in blocks of 32 columns (32 / G queries, the group's G heads of each side by side), the B operand of
@@ -301,9 +303,11 @@ constexpr int kStageBytes = 8 * 1024 + 256;       // 32 columns of 256 bytes, an
 constexpr int kGroup = HS_MASS_TILES;
 constexpr int kAhead = 2;                         // pairs of exponentials in front of a block's first products
 // Products of a block beside the exponentials of the one before (two sets of scores), or one set and, for the registers that this frees, 3 waves per
-// SIMD instead of 2 (dense keys).  us, beside / one set: dense keys per tile, 4096 queries on 16K tokens 470 / 460, 512 on 4 x 4K 85 / 81, a 2K prompt
-// 39 / 33, 100 queries on 32K 41 / 40; per token 481 / 592 (registers spilled).  2:4 keys, 3 waves either way, per tile: 4096 queries 366 / 362, 128 on 32K
-// 37.8 / 36.6, a 16K prompt 802 / 817, a 2K one 31 / 32.5; per token 423 / 432, a 16K prompt 918 / 957.
+// SIMD instead of 2 (dense keys, and 2:4 ones per token).  us, beside / one set, on one card: dense keys per tile, 4096 queries on 16K tokens 491 / 478, 512
+// on 4 x 4K 79 / 78, a 2K prompt 36.7 / 31.7, a 16K one 1026 / 1021, 100 queries on 32K 39.1 / 39.3; per token 4096 queries 500 / 615, a 16K prompt 1048 / 1262
+// (55 registers spilled; beside, one).  2:4 keys per tile, 3 waves either way: 4096 queries 369 / 365, 128 on 32K 37.7 / 36.5, 512 on 4 x 4K 65 / 62, a 16K
+// prompt 813 / 826, a 2K one 29.2 / 31.6; per token 4096 queries 400 / 409, 128 on 32K 40.2 / 41.0, 512 on 4 x 4K 73 / 73, a 16K prompt 864 / 899, a 2K one
+// 37.7 / 32.6.
 constexpr bool beside(bool token, bool dense) { return token || !dense; }
 
 // A block's 32 columns lie in LDS one after the other, the 16-byte chunks of column r exchanged by c -> c ^ (r & 15): loads from memory are of
