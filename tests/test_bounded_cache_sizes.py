@@ -226,3 +226,94 @@ def test_binding_refuses_numbers_that_are_no_int32():
                      lambda: hb.keep_tokens(sh, K, K, w, 2, last=big), lambda: hb.rope_qkv(sh, rope, q[:, :1].expand(1, (1 << 31) + 5, 4, D))):
             with pytest.raises(hb.HsError, match="32-bit"):
                 call()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# evicted caches of many tiles, captured calls of long rows
+# ---------------------------------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("sk,sv,B,Hkv,T,keep", [(1.0, 1.0, 1, 8, 1024, 300), (0.5, 1.0, 2, 4, 512, 130), (0.97, 0.5, 1, 2, 2500, 2000), (1.0, 1.0, 16, 8, 40, 7)])
+def test_attention_over_a_large_cache_after_eviction(sk, sv, B, Hkv, T, keep):
+    """Slots in no order, pools that say nothing is skipped: decode (tiles by range and by count, with a tail and without) and prefill give the bits of a cache
+    into which only the remaining tiles were packed, in order, with pools of the same sizes."""
+    G, L = 4, T * TILE
+    gd = torch.Generator(device="cuda").manual_seed(T)
+    K, V = (torch.randn((B, Hkv, L, D), generator=gd, device="cuda").bfloat16() for _ in range(2))
+    sh = hb.make_shape(B, Hkv * G, Hkv, L)
+    kv = hb.compress_kv(sh, hb.make_policy(sparse_frac_k=sk, sparse_frac_v=sv), K, V)
+    states = [np.where(m > 0, hb.DENSE, hb.SPARSE24).astype(np.int8) for m in (kv.k_map.cpu().numpy(), kv.v_map.cpu().numpy())]
+    hb.evict_tiles(sh, kv, torch.rand((B, Hkv, T), generator=gd, device="cuda"), keep, first=1, last=4)
+    gone = (kv.k_map == 0).cpu().numpy()
+    assert (gone.sum(-1) == T - keep).all()
+    slots = kv.k_map[0, 0].cpu().numpy()
+    slots = -slots[slots < 0]
+    assert (np.sort(slots) == np.arange(1, len(slots) + 1)).all() and (np.diff(slots) < 0).any()
+    for s in states:
+        s[gone] = hb.SKIP
+    fresh = hb.PackedKV(sh, kv.counts, "cuda")
+    pol = hb.make_policy(state_k=states[0], state_v=states[1])
+    hb.compress_kv(sh, pol, K, V, out=fresh)
+    hb.check_state_flag(pol)
+    Q = torch.randn((B, Hkv * G, 192, D), generator=gd, device="cuda").bfloat16()
+    tk, tv = (torch.randn((B, Hkv, TILE, D), generator=gd, device="cuda").bfloat16() for _ in range(2))
+    for Lq in (64, 192):
+        for a, b in zip(hb.prefill_attn(sh, Q[:, :, :Lq].contiguous(), kv), hb.prefill_attn(sh, Q[:, :, :Lq].contiguous(), fresh)):
+            assert torch.equal(a, b)
+    q = Q[:, :, 0].contiguous()
+    for extra in (dict(), dict(tail_k=tk, tail_v=tv, tail_len=33)):
+        for a, b in zip(hb.decode_attn(sh, q, kv, **extra), hb.decode_attn(sh, q, fresh, **extra)):
+            assert torch.equal(a, b)
+    lse = torch.full((B, Hkv * G, 192), math.log(keep * TILE), device="cuda")
+    for per_token in (False, True):
+        assert torch.equal(hb.attn_mass(sh, Q, lse, kv, per_token=per_token), hb.attn_mass(sh, Q, lse, fresh, per_token=per_token))
+
+
+@gpu
+def test_captured_calls_of_long_rows_replay():
+    """Rows in parts, held tiles numbered in several ranges, many tiles dropped: captured once, replayed with other inputs, eager work between the replays."""
+    B, Hkv, G, T, n, Lq = 2, 2, 4, 150, 30000, 1000
+    L = T * TILE
+    gd = torch.Generator(device="cuda").manual_seed(3)
+    sh = hb.make_shape(B, Hkv * G, Hkv, L)
+    K = torch.randn((B, Hkv, n, D), generator=gd, device="cuda").bfloat16()
+    kv = hb.compress_kv(sh, hb.make_policy(sparse_frac_k=0.5), K[:, :, :L], K[:, :, L:2 * L])
+    kv.uniform = 0
+    Q, lse = torch.empty((B, Hkv * G, Lq, D), dtype=torch.bfloat16, device="cuda"), torch.empty((B, Hkv * G, Lq), device="cuda")
+    w, mass = torch.empty((B, Hkv, n), device="cuda"), torch.empty((B, Hkv, T), device="cuda")
+    bufs = [t for t in (kv.k_dense, kv.k_nnz, kv.k_meta, kv.k_map, kv.v_dense, kv.v_nnz, kv.v_meta, kv.v_map) if t is not None]
+    backup = [t.clone() for t in bufs]
+    assert hb.attn_mass_workspace_bytes(sh, Lq) > mass.nbytes
+
+    def fill():
+        Q.normal_(generator=gd), lse.uniform_(8.0, 10.0, generator=gd), w.exponential_(generator=gd), mass.uniform_(generator=gd)
+        for t, b in zip(bufs, backup):
+            t.copy_(b)
+
+    def calls():
+        hb.attn_mass(sh, Q, lse, kv, mass=mass, decay=0.5)
+        kept = hb.keep_tokens(sh, K, K, w, 2000, first=4, last=32)
+        hb.evict_tiles(sh, kv, mass, 60, first=1, last=2)
+        return [mass, *kept, *bufs]
+
+    fill()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    fill()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls()
+    for _ in range(4):
+        fill()
+        before = mass.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        mass.copy_(before)
+        for t, b in zip(bufs, backup):
+            t.copy_(b)
+        for a, b in zip(got, calls()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
