@@ -467,6 +467,56 @@ HS_API int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view
                    const int64_t weight_strides[2], const int32_t* lens, int32_t keep, int32_t first, int32_t last, void* K_out,
                    void* V_out, int32_t* index, void* workspace, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Tiles picked for each query: the cache stays whole, and a query reads the part of it that a cheap score picks.  Bounds of a tile's keys are
+ * made once, when it is filled; a step scores all tiles by them, picks some, and attends to these.  Extensions of this library, in its own
+ * terms.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Per tile, kv head and channel the smallest and the largest key, as the cache holds them (a pruned entry is 0).
+ *   bounds   device, 16 bit [B, Hkv, L / 64, 2, D], 16-byte aligned: the smallest, then the largest.  Values of the keys, bit for bit, by the order
+ *            of their encoding: -NaN, -inf .. -0, +0 .. inf, +NaN.  A tile that is SKIP gets zeros.
+ * Of every (b, kv head) row the tiles tile .. tile + n_tiles - 1 (0 <= tile, n_tiles >= 1, tile + n_tiles <= L / 64); or, tiles not NULL: device
+ * int32 [B], of batch row b tile tiles[b] alone (as hs_append_tile_rows fills it; any value outside 0 .. L / 64 - 1 leaves the row as it is; tile and
+ * n_tiles are not looked at).  Bounds of other tiles are left as they are.  B Hkv n_tiles <= 2^26 - 4 (HS_EUNSUPPORTED beyond).  They hold until
+ * the tile's keys change: hs_append_tile and hs_recompress_kv make new ones necessary, hs_evict_tiles does not. */
+HS_API int hs_tile_bounds(const hs_shape* shape, int32_t tile, int32_t n_tiles, const int32_t* tiles, const hs_kv* kv, void* bounds, void* stream);
+
+/* What a query can score at most in a tile, for every (b, kv head), query and tile:
+ *   scores = max over the group's Hq / Hkv heads of  sum over the channels c of  max(q_c, 0) largest_c + min(q_c, 0) smallest_c,
+ * in units of q . k (a scale > 0 does not change the order), fp32.  NaN counts as +inf: such a tile cannot be ruled out.  -inf: tiles that are SKIP
+ * (k_map: the cache's K map, device int32 [B, Hkv, L / 64], 0 = SKIP; NULL: no tile is), and causal those that begin behind the query.
+ *   Q       [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i (0 <= q_start, q_start + Lq <= L if causal, else q_start is not looked at)
+ *   scores  [B, Hkv, Lq, L / 64] contiguous
+ * HS_EUNSUPPORTED beyond 2^24 - 1 workgroups of 64 tiles by (up to) 16 queries.  No workspace. */
+HS_API int hs_query_scores(const hs_shape* shape, int32_t Lq, int32_t q_start, int causal, const hs_view* Q, const void* bounds, const int32_t* k_map,
+                    float* scores, void* stream);
+
+/* Picks tiles for each query by scores [B, Hkv, Lq, L / 64] (contiguous): of the tiles with a score above -inf the first `first`, the last `last`, and of
+ * the others those of largest score, n_pick in all (NaN counts as +inf; ties and equal zeros: the lower tile first).
+ *   list  device int32 [B, Hkv, Lq, n_pick]: the tiles, ascending, then -1
+ * n_pick >= 1, n_pick >= first + last; L / 64 <= 65536, n_pick <= 2^20 and B Hkv Lq < 2^22 (HS_EUNSUPPORTED beyond).  No workspace. */
+HS_API int hs_pick_tiles(const hs_shape* shape, int32_t Lq, const float* scores, int32_t n_pick, int32_t first, int32_t last, int32_t* list, void* stream);
+
+/* Attention of each query over the tiles that its list names: what hs_prefill_attn_at and the decode calls compute, of a cache whose other tiles
+ * were SKIP for this query.  All heads of a group share the list.
+ *   Q     [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i (as for hs_query_scores) and, causal, sees tokens up to that
+ *   list  device int32 [B, Hkv, Lq, n_list]: tiles in any order; one named more than once counts once, numbers outside 0 .. L / 64 - 1 and tiles
+ *         that are SKIP are passed over
+ *   tail  the dense tail of a decode step (Lq == 1, causal 0): tail_k, tail_v [B, Hkv, 64, D] contiguous or both NULL, tail_len tokens valid
+ *         (tail_lens: device int32 [B] instead, clamped into 0 .. 64); it is attended to whatever the list says
+ *   O     [B, Hq, Lq, D], LSE fp32 [B, Hq, Lq] or NULL, contiguous.  Nothing seen: O = 0, LSE = -inf; a score that is NaN: O = NaN, LSE = NaN.
+ *         Keys and values that a query does not see do not touch its results, infinities and NaN among them.
+ * scale as for hs_prefill_attn.  L / 64 <= 65536, B Hkv (Lq + 1) < 2^23 (HS_EUNSUPPORTED beyond).  workspace: hs_listed_attn_workspace_bytes
+ * bytes, 16-byte aligned (NULL where that is 0), not shared between two calls in flight; no initial content.  Equal calls give equal bits, and so do lists
+ * that name the same tiles with the same n_list. */
+HS_API int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q, const hs_kv* kv,
+                   const int32_t* list, int32_t n_list, const void* tail_k, const void* tail_v, int32_t tail_len, const int32_t* tail_lens,
+                   void* O, float* LSE, void* workspace, void* stream);
+
+/* Its workspace: 0 where the queries fill the GPU.  [host, pure] */
+HS_API int hs_listed_attn_workspace_bytes(const hs_shape* shape, int32_t Lq, int32_t n_list, int with_tail, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -115,6 +115,12 @@ EXPORTS = {
                                  C.c_void_p, C.c_void_p]),
     "hs_keep_tokens": (C.c_int, [C.POINTER(HsShape), C.c_int32, _VIEW, _VIEW, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p, C.c_int32,
                                  C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hs_tile_bounds": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int32, C.c_void_p, C.POINTER(HsKV), C.c_void_p, C.c_void_p]),
+    "hs_query_scores": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int32, C.c_int, _VIEW, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hs_pick_tiles": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+    "hs_listed_attn": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int32, C.c_float, C.c_int, _VIEW, C.POINTER(HsKV), C.c_void_p, C.c_int32,
+                                 C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hs_listed_attn_workspace_bytes": (C.c_int, [C.POINTER(HsShape), C.c_int32, C.c_int32, C.c_int, C.POINTER(C.c_size_t)]),
     "hs_decode_attn_phases": (C.c_int, [C.POINTER(HsShape), C.c_float, C.c_int32, C.c_void_p, C.POINTER(HsKV),
                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int]),
 }
@@ -140,11 +146,13 @@ def lib():
 _NATIVE_ENTRIES = ("hs_kv_bytes", "hs_workspace_bytes", "hs_decode_auto_splits", "hs_decode_attn", "hs_decode_attn_static",
                    "hs_decode_attn_tail", "hs_decode_attn_tail_rows", "hs_prefill_plan", "hs_prefill_attn_ws",
                    "hs_append_tiles", "hs_append_tile_rows", "hs_tile_counts", "hs_compress_kv", "hs_recompress_kv", "hs_rope_qkv", "hs_attn_mass",
-                   "hs_attn_mass_workspace_bytes", "hs_evict_tiles", "hs_keep_tokens")
+                   "hs_attn_mass_workspace_bytes", "hs_evict_tiles", "hs_keep_tokens", "hs_tile_bounds", "hs_query_scores", "hs_pick_tiles", "hs_listed_attn",
+                   "hs_listed_attn_workspace_bytes")
 
 
 # what calls it
-_NATIVE_CALLS = ("decode", "decode_static", "prefill", "append", "pools", "compress", "recompress", "rope", "mass", "evict", "keep")
+_NATIVE_CALLS = ("decode", "decode_static", "prefill", "append", "pools", "compress", "recompress", "rope", "mass", "evict", "keep", "bounds",
+                 "scores", "pick", "listed")
 
 
 def _load_native(L):
@@ -770,6 +778,132 @@ def keep_tokens(shape, K, V, weight, keep, first=0, last=0, lens=None):
                                 (C.c_int64 * 2)(weight.stride(0), weight.stride(1)), at, keep, first, last, _ptr(K_out), _ptr(V_out),
                                 _ptr(index), _ptr(workspace), _stream()))
     return K_out, V_out, index
+
+
+# ---- tiles picked for each query: bounds of the keys, scores, the choice, attention over listed tiles ----
+
+def tile_bounds(shape, kv, tile=0, n_tiles=None, out=None):
+    """Per tile, kv head and channel the smallest and the largest key of the packed cache: [B, Hkv, L / 64, 2, D] of the cache's type, zeros for
+    tiles that are SKIP.  For the tiles tile .. tile + n_tiles - 1 (default: to the end), or, tile an int32 device tensor [B], for tile tile[b] of each
+    sequence alone (others than 0 .. L / 64 - 1: none).  out: the bounds made so far, whose other tiles stay (default: new ones, zeros there)."""
+    r = _done(_fast().bounds(shape, kv, tile, n_tiles, out))
+    if r is not None:
+        return r
+    T = shape.L // TILE
+    _here(kv.k_map, out)
+    rows = _int32(tile, (shape.B,)) if torch.is_tensor(tile) else None
+    if rows is not None:
+        _here(tile)
+    first = 0 if rows is not None else _i32(tile)
+    n = _i32((T - first if rows is None else 1) if n_tiles is None else n_tiles)
+    sizes = (shape.B, shape.Hkv, T, 2, shape.D)
+    assert out is None or (out.dtype == torch_dtype(shape) and tuple(out.shape) == sizes and out.is_contiguous())
+    if out is None:
+        whole = rows is None and first == 0 and n == T
+        out = (torch.empty if whole else torch.zeros)(sizes, dtype=torch_dtype(shape), device=kv.k_map.device)
+    kvs = kv.struct()
+    _check(lib().hs_tile_bounds(C.byref(shape), first, n, rows, C.byref(kvs), _ptr(out), _stream()))
+    return out
+
+
+def query_scores(shape, Q, bounds, k_map=None, causal=None, q_start=None, out=None):
+    """What each query of Q [B, Hq, Lq, D] (or [B, Hq, D]: one per head) can score at most in each tile, by the tiles' bounds (tile_bounds): the largest
+    of the group's heads, in units of q . k, fp32 [B, Hkv, Lq, L / 64] (or [B, Hkv, L / 64]); -inf for tiles that are SKIP in k_map (the cache's K map;
+    None: none is) and, causal (default: for queries with a token axis), for those that begin behind the query.  Views of Q are taken.  q_start: as for
+    prefill_attn."""
+    r = _done(_fast().scores(shape, Q, bounds, k_map, causal, q_start, out))
+    if r is not None:
+        return r
+    one, T = Q.dim() == 3, shape.L // TILE
+    if causal is None:
+        causal = not one
+    if one:
+        Q = Q.unsqueeze(2)
+    Lq = _i32(Q.shape[2])
+    at = _i32(shape.L - Lq if q_start is None else q_start) if causal else 0
+    _here(Q, bounds, k_map, out)
+    assert Q.dtype == torch_dtype(shape) and tuple(Q.shape) == (shape.B, shape.Hq, Lq, shape.D)
+    assert bounds.dtype == Q.dtype and tuple(bounds.shape) == (shape.B, shape.Hkv, T, 2, shape.D) and bounds.is_contiguous()
+    held = None if k_map is None else _int32(k_map, (shape.B, shape.Hkv, T))
+    sizes = (shape.B, shape.Hkv, T) if one else (shape.B, shape.Hkv, Lq, T)
+    assert out is None or (out.dtype == torch.float32 and tuple(out.shape) == sizes and out.is_contiguous())
+    if out is None:
+        out = Q.new_empty(sizes, dtype=torch.float32)
+    _check(lib().hs_query_scores(C.byref(shape), Lq, at, int(bool(causal)), C.byref(_view(Q, 1, 2)), _ptr(bounds), held, _ptr(out), _stream()))
+    return out
+
+
+def pick_tiles(shape, scores, n, first=0, last=0, out=None):
+    """The n tiles that each query attends to, by scores [B, Hkv, Lq, L / 64] (or [B, Hkv, L / 64]): of the tiles with a score above -inf the first
+    `first`, the last `last`, and of the others those of largest score.  int32 [B, Hkv, Lq, n] (or [B, Hkv, n]), ascending, then -1."""
+    r = _done(_fast().pick(shape, scores, n, first, last, out))
+    if r is not None:
+        return r
+    n, first, last = _i32(n), _i32(first), _i32(last)
+    _here(scores, out)
+    assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.dim() in (3, 4)
+    assert tuple(scores.shape[:2]) == (shape.B, shape.Hkv) and scores.shape[-1] == shape.L // TILE
+    Lq = 1 if scores.dim() == 3 else _i32(scores.shape[2])
+    if n < 1:
+        raise HsError("pick_tiles: at least one tile is picked")
+    sizes = tuple(scores.shape[:-1]) + (n,)
+    assert out is None or (out.dtype == torch.int32 and tuple(out.shape) == sizes and out.is_contiguous())
+    if out is None:
+        out = scores.new_empty(sizes, dtype=torch.int32)
+    _check(lib().hs_pick_tiles(C.byref(shape), Lq, _ptr(scores), n, first, last, _ptr(out), _stream()))
+    return out
+
+
+def listed_attn_workspace_bytes(shape, Lq, n, with_tail=False):
+    """Scratch that listed_attn takes for this call."""
+    need = C.c_size_t(0)
+    _check(lib().hs_listed_attn_workspace_bytes(C.byref(shape), _i32(Lq), _i32(n), int(bool(with_tail)), C.byref(need)))
+    return need.value
+
+
+def listed_attn(shape, Q, kv, tiles, causal=None, scale=0.0, q_start=None, tail_k=None, tail_v=None, tail_len=None, want_lse=True, out=None, lse=None,
+                workspace=None):
+    """Attention of each query of Q [B, Hq, Lq, D] (or [B, Hq, D]: one per head) over the tiles of the packed cache that its list names: tiles int32
+    [B, Hkv, Lq, n] (or [B, Hkv, n]; see pick_tiles), in any order; numbers that are no tiles (-1) and tiles that are SKIP are passed over, one named
+    twice counts once.  causal (default: for queries with a token axis), scale, q_start: as for prefill_attn.  tail_k, tail_v [B, Hkv, 64, D] with tail_len
+    (int or int32 device tensor [B]): the dense tail of a decode step.  Views of Q are taken.  Returns (O, LSE fp32 or None), shaped as the queries."""
+    r = _fast().listed(shape, Q, kv, tiles, causal, scale, q_start, tail_k, tail_v, tail_len, want_lse, out, lse, workspace)
+    if r is not None:
+        return _done(r)
+    one = Q.dim() == 3
+    if causal is None:
+        causal = not one
+    if one:
+        Q = Q.unsqueeze(2)
+    Lq, n = _i32(Q.shape[2]), _i32(tiles.shape[-1])
+    at = _i32(shape.L - Lq if q_start is None else q_start) if causal else 0
+    n_tail = 0 if tail_len is None or torch.is_tensor(tail_len) else _i32(tail_len)
+    _here(Q, tiles, tail_k, tail_v, out, lse, workspace, kv.k_map)
+    assert Q.dtype == torch_dtype(shape) and tuple(Q.shape) == (shape.B, shape.Hq, Lq, shape.D)
+    _int32(tiles, (shape.B, shape.Hkv, n) if one else (shape.B, shape.Hkv, Lq, n))
+    sizes = (shape.B, shape.Hq, shape.D) if one else (shape.B, shape.Hq, Lq, shape.D)
+    assert out is None or (out.dtype == Q.dtype and tuple(out.shape) == sizes and out.is_contiguous())
+    assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == sizes[:-1] and lse.is_contiguous())
+    lens = None
+    assert (tail_k is None) == (tail_v is None) and (tail_k is None) == (tail_len is None)
+    if tail_k is not None:
+        for t in (tail_k, tail_v):
+            assert t.dtype == Q.dtype and t.is_contiguous() and tuple(t.shape) == (shape.B, shape.Hkv, TILE, shape.D)
+        if torch.is_tensor(tail_len):
+            _here(tail_len)
+            lens = _int32(tail_len, (shape.B,))
+    if out is None:
+        out = Q.new_empty(sizes)
+    if lse is None and want_lse:
+        lse = Q.new_empty(sizes[:-1], dtype=torch.float32)
+    need = listed_attn_workspace_bytes(shape, Lq, n, tail_k is not None)
+    if workspace is None:
+        workspace = _workspace(need, Q.device) if need else None
+    assert workspace is None or workspace.nbytes >= need
+    kvs = kv.struct()
+    _check(lib().hs_listed_attn(C.byref(shape), Lq, at, float(scale), int(bool(causal)), C.byref(_view(Q, 1, 2)), C.byref(kvs), _ptr(tiles), n,
+                                _ptr(tail_k), _ptr(tail_v), n_tail, lens, _ptr(out), _ptr(lse), _ptr(workspace), _stream()))
+    return out, lse
 
 
 def bits_to_bf16_tensor(bits, device="cuda", dtype=torch.bfloat16):

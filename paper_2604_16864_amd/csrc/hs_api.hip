@@ -765,3 +765,112 @@ int hs_keep_tokens(const hs_shape* shape, int32_t n_tokens, const hs_view* K, co
 }
 
 }  // extern "C"
+
+// -------- tiles picked for each query --------
+namespace {
+
+// queries of a call on a cache: how many, and where they stand
+int check_queries(const hs_shape* s, int32_t Lq, int32_t q_start, int causal) {
+  if (Lq < 1) return HS_EINVAL;
+  if (Lq > 1 << 30) return HS_EUNSUPPORTED;
+  if (causal && (q_start < 0 || Lq > s->L || q_start > s->L - Lq)) return HS_EINVAL;
+  return HS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hs_tile_bounds(const hs_shape* shape, int32_t tile, int32_t n_tiles, const int32_t* tiles, const hs_kv* kv, void* bounds, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  rc = check_kv(shape, kv);
+  if (rc != HS_OK) return rc;
+  const int T = shape->L / HS_BT;
+  if (bounds == nullptr || ((uintptr_t)bounds & 15u)) return HS_EINVAL;
+  if (tiles != nullptr) { tile = 0; n_tiles = 1; }
+  if (tile < 0 || n_tiles < 1 || n_tiles > T || tile > T - n_tiles) return HS_EINVAL;
+  if ((int64_t)shape->B * shape->Hkv * n_tiles > (int64_t)HS_BOUNDS_TILES * HS_MAX_BLOCKS) return HS_EUNSUPPORTED;
+  const hipError_t e = hs_launch_bounds(shape->B, shape->Hkv, T, hs_make_kv_dev(kv), tile, n_tiles, tiles, (uint16_t*)bounds, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_query_scores(const hs_shape* shape, int32_t Lq, int32_t q_start, int causal, const hs_view* Q, const void* bounds, const int32_t* k_map,
+                    float* scores, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  rc = check_queries(shape, Lq, q_start, causal);
+  if (rc != HS_OK) return rc;
+  if (Q == nullptr || bounds == nullptr || ((uintptr_t)bounds & 15u) || scores == nullptr || (((uintptr_t)scores | (uintptr_t)k_map) & 3u)) return HS_EINVAL;
+  hs_scores_args a = {};
+  rc = view_of(Q, shape->B, shape->Hq, Lq, false, &a.q);
+  if (rc != HS_OK) return rc;
+  a.bounds = (const uint16_t*)bounds; a.k_map = k_map; a.scores = scores;
+  a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.T = shape->L / HS_BT;
+  a.Lq = Lq; a.q_start = q_start; a.causal = causal != 0;
+  if (hs_scores_blocks(a) > HS_MAX_BLOCKS) return HS_EUNSUPPORTED;
+  const hipError_t e = hs_launch_scores(a, shape->dtype, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_pick_tiles(const hs_shape* shape, int32_t Lq, const float* scores, int32_t n_pick, int32_t first, int32_t last, int32_t* list, void* stream) {
+  const int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  const int T = shape->L / HS_BT;
+  if (Lq < 1 || scores == nullptr || list == nullptr || (((uintptr_t)scores | (uintptr_t)list) & 3u)) return HS_EINVAL;
+  if (n_pick < 1 || first < 0 || last < 0 || (int64_t)first + last > n_pick) return HS_EINVAL;
+  const int64_t rows = (int64_t)shape->B * shape->Hkv * Lq;
+  if (T > kSelectMaxTiles || n_pick > 1 << 20 || rows > HS_MAX_BLOCKS / 4) return HS_EUNSUPPORTED;
+  const hipError_t e = hs_launch_pick(rows, T, scores, n_pick, first, last, list, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+int hs_listed_attn_workspace_bytes(const hs_shape* shape, int32_t Lq, int32_t n_list, int with_tail, size_t* bytes) {
+  const int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  if (Lq < 1 || n_list < 1 || bytes == nullptr) return HS_EINVAL;
+  *bytes = (size_t)hs_listed_parts(shape->B, shape->Hkv, Lq, n_list, with_tail != 0) * shape->B * shape->Hq * Lq * (HS_D + 1) * sizeof(float);
+  return HS_OK;
+}
+
+int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q, const hs_kv* kv, const int32_t* list,
+                   int32_t n_list, const void* tail_k, const void* tail_v, int32_t tail_len, const int32_t* tail_lens, void* O, float* LSE,
+                   void* workspace, void* stream) {
+  int rc = check_shape(shape);
+  if (rc != HS_OK) return rc;
+  rc = check_kv(shape, kv);
+  if (rc != HS_OK) return rc;
+  rc = check_queries(shape, Lq, q_start, causal);
+  if (rc != HS_OK) return rc;
+  if (Q == nullptr || list == nullptr || ((uintptr_t)list & 3u) || n_list < 1 || O == nullptr || ((uintptr_t)O & 1u) || ((uintptr_t)LSE & 3u)) return HS_EINVAL;
+  if (!(scale >= 0.f)) return HS_EINVAL;
+  if ((tail_k == nullptr) != (tail_v == nullptr)) return HS_EINVAL;
+  if (tail_k != nullptr) {
+    if (Lq != 1 || causal) return HS_EUNSUPPORTED;
+    if ((((uintptr_t)tail_k | (uintptr_t)tail_v) & 15u) || (tail_lens == nullptr && (tail_len < 0 || tail_len > HS_BT))) return HS_EINVAL;
+  }
+  const int T = shape->L / HS_BT;
+  if (kv->uniform) {
+    const bool k_ok = (kv->cap_dense_k == 0 && kv->cap_sparse_k >= T) || (kv->cap_sparse_k == 0 && kv->cap_dense_k >= T);
+    const bool v_ok = (kv->cap_dense_v == 0 && kv->cap_sparse_v >= T) || (kv->cap_sparse_v == 0 && kv->cap_dense_v >= T);
+    if (!k_ok || !v_ok) return HS_EINVAL;
+  }
+  hs_listed_args a = {};
+  rc = view_of(Q, shape->B, shape->Hq, Lq, false, &a.q);
+  if (rc != HS_OK) return rc;
+  if (T > kSelectMaxTiles) return HS_EUNSUPPORTED;
+  const int64_t blocks = (int64_t)shape->B * shape->Hkv * ((int64_t)Lq * hs_listed_splits(shape->B, shape->Hkv, Lq, n_list) + 1);
+  if (blocks > HS_MAX_BLOCKS / 2) return HS_EUNSUPPORTED;
+  if (hs_listed_parts(shape->B, shape->Hkv, Lq, n_list, tail_k != nullptr) > 0 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
+  a.list = list;
+  a.tail_k = (const uint16_t*)tail_k; a.tail_v = (const uint16_t*)tail_v; a.tail_lens = tail_lens;
+  a.tail_len = tail_k == nullptr ? -1 : (tail_lens != nullptr ? 0 : tail_len);
+  a.o = (uint16_t*)O; a.lse = LSE; a.ws = (float*)workspace;
+  a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.T = T;
+  a.Lq = Lq; a.q_start = q_start; a.causal = causal != 0; a.n_list = n_list;
+  a.scale = scale == 0.f ? 1.0f / sqrtf((float)HS_D) : scale;
+  const hipError_t e = hs_launch_listed(a, hs_make_kv_dev(kv), shape->dtype, (hipStream_t)stream);
+  return e != hipSuccess ? hip_fail(e) : HS_OK;
+}
+
+}  // extern "C"

@@ -254,3 +254,35 @@ enum { HS_KEEP_GATHERED = 16 };  // output rows of a workgroup that gathers: kee
 size_t hs_keep_ws_bytes(int64_t rows, int n);
 hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, const float* weight, int64_t w_sb, int64_t w_sh, const int32_t* lens,
                           int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, void* ws, hipStream_t st);
+
+// -------- tiles picked for each query --------
+enum { HS_BOUNDS_TILES = 4 };  // tiles of a workgroup: B Hkv n_tiles <= HS_BOUNDS_TILES * HS_MAX_BLOCKS
+hipError_t hs_launch_bounds(int B, int Hkv, int T, const hs_kv_dev& kv, int tile, int n_tiles, const int32_t* tiles, uint16_t* bounds, hipStream_t st);
+struct hs_scores_args {
+  hs_vec_view q;
+  const uint16_t* bounds;
+  const int32_t* k_map;
+  float* scores;
+  int32_t B, Hq, Hkv, T, Lq, q_start, causal;
+};
+// workgroups of a call; at most HS_MAX_BLOCKS are launched
+int64_t hs_scores_blocks(const hs_scores_args& a);
+hipError_t hs_launch_scores(const hs_scores_args& a, int dtype, hipStream_t st);
+// rows of T <= 65536 scores, rows <= HS_MAX_BLOCKS / 4
+hipError_t hs_launch_pick(int64_t rows, int T, const float* scores, int n_pick, int first, int last, int32_t* list, hipStream_t st);
+struct hs_listed_args {
+  hs_vec_view q;
+  const int32_t* list;
+  const uint16_t *tail_k, *tail_v;
+  const int32_t* tail_lens;
+  uint16_t* o;
+  float* lse;
+  float* ws;
+  int32_t B, Hq, Hkv, T, Lq, q_start, causal, n_list, tail_len;  // tail_len < 0: no tail
+  float scale;
+};
+// ranges that a query's list is cut into; with more than one (or one, and a tail that is a part of its own) the parts go through ws:
+// hs_listed_parts * B * Hq * Lq * 129 floats, 0 parts: none
+int hs_listed_splits(int B, int Hkv, int Lq, int n_list);
+int hs_listed_parts(int B, int Hkv, int Lq, int n_list, int with_tail);
+hipError_t hs_launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);

@@ -1,5 +1,5 @@
 // Argument marshalling of the Python binding in native code: the per-call part of decode, prefill, append, compress,
-// re-compress and of the calls around a bounded cache.  What a call on a small cache costs is mostly this part: in Python with ctypes a decode call of 7 us of
+// re-compress, of the calls around a bounded cache and of those that pick tiles for each query.  What a call on a small cache costs is mostly this part: in Python with ctypes a decode call of 7 us of
 // kernels took 13.3 us (8 data_ptr() calls and a ctypes structure for the cache, three allocations, two library calls) and takes
 // 9 here, compressing 2K tokens 16.1 and 8.5.
 //
@@ -45,6 +45,11 @@ struct Entries {  // of libhs.so, as the binding has loaded it
   decltype(&hs_attn_mass_workspace_bytes) mass_bytes;
   decltype(&hs_evict_tiles) evict;
   decltype(&hs_keep_tokens) keep;
+  decltype(&hs_tile_bounds) bounds;
+  decltype(&hs_query_scores) scores;
+  decltype(&hs_pick_tiles) pick;
+  decltype(&hs_listed_attn) listed;
+  decltype(&hs_listed_attn_workspace_bytes) listed_bytes;
 } g_hs;
 PyTypeObject *g_shape_type, *g_policy_type, *g_kv_type, *g_rope_type;
 
@@ -702,6 +707,191 @@ PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- tiles picked for each query ----
+
+// whether a cache's maps are tensors on the current device
+bool cache_here(PyObject* cache, bool* ok) {
+  PyObject* map = PyObject_GetAttr(cache, g_names[S_K_MAP]);
+  if (map == nullptr) return false;
+  *ok = exact_tensor(map) && here(tensor(map));
+  Py_DECREF(map);
+  return true;
+}
+// queries [B, Hq, Lq, D], or [B, Hq, D] (one), and where they stand; causal: None, True or False
+struct Queries { bool one; int64_t n; int causal; int32_t q_start; hs_view view; };
+bool queries_of(PyObject* o, PyObject* causal, PyObject* q_start, const hs_shape& s, Queries* r) {
+  if (!exact_tensor(o) || !(causal == Py_None || PyBool_Check(causal))) return false;
+  const at::Tensor& q = tensor(o);
+  r->one = q.dim() == 3;
+  if ((!r->one && q.dim() != 4) || q.scalar_type() != element_type(s) || !here(q)) return false;
+  r->n = r->one ? 1 : q.size(2);
+  if (r->n > INT32_MAX || q.size(0) != s.B || q.size(1) != s.Hq || q.size(q.dim() - 1) != s.D || q.stride(q.dim() - 1) != 1) return false;
+  r->causal = causal == Py_None ? !r->one : causal == Py_True;
+  r->q_start = 0;
+  if (r->causal) {
+    r->q_start = s.L - (int32_t)r->n;
+    if (q_start != Py_None && !get_int(q_start, &r->q_start)) return false;
+  }
+  r->view = r->one ? hs_view{q.data_ptr(), q.stride(0), q.stride(1), 0} : view(q, 1, 2);
+  return true;
+}
+PyObject* kept_or_made(PyObject* kept, const at::Tensor& made) {
+  if (kept == Py_None) return THPVariable_Wrap(made);
+  Py_INCREF(kept);
+  return kept;
+}
+
+// bounds(shape, cache, tile, n_tiles, out) -> out.  Bounds of a part of the tiles into no tensor yet are the binding's.
+PyObject* bounds(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  hs_kv kv;
+  int32_t tile, n_tiles;
+  const int32_t* tiles;
+  if (n_args != 5 || !get_shape(a[0], &s) || !none_or_tensor(a[4]) || s.L < 64 || !int_or_rows(a[2], {s.B}, &tile, &tiles) || !get_kv(a[1], &kv))
+    Py_RETURN_NONE;
+  bool ok;
+  if (!cache_here(a[1], &ok)) return nullptr;
+  if (!ok) Py_RETURN_NONE;
+  const int32_t T = s.L / 64;
+  n_tiles = tiles != nullptr ? 1 : (tile >= 0 && tile < T ? T - tile : 0);
+  if (a[3] != Py_None && !get_int(a[3], &n_tiles)) Py_RETURN_NONE;
+  const bool own = a[4] == Py_None;
+  if (own && (tiles != nullptr || tile != 0 || n_tiles != T)) Py_RETURN_NONE;
+  const int64_t sizes[5] = {s.B, s.Hkv, T, 2, s.D};
+  if (!own && !whole(tensor(a[4]), element_type(s), sizes)) Py_RETURN_NONE;
+  void* out_ptr = address(a[4]);
+  PyObject* map = own ? PyObject_GetAttr(a[1], g_names[S_K_MAP]) : nullptr;
+  if (own && map == nullptr) return nullptr;
+  at::Tensor out, like;
+  if (own) { like = tensor(map); Py_DECREF(map); }
+  int rc;
+  {
+    NoGil others_run;
+    if (own) { out = NewTensors(like)(sizes, element_type(s)); out_ptr = out.data_ptr(); }
+    rc = g_hs.bounds(&s, tile, n_tiles, tiles, &kv, out_ptr, current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  return kept_or_made(a[4], out);
+  END_HANDLE_TH_ERRORS
+}
+
+// scores(shape, Q, bounds, k_map, causal, q_start, out) -> out
+PyObject* scores(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  Queries q;
+  if (n_args != 7 || !get_shape(a[0], &s) || !exact_tensor(a[2]) || !none_or_tensor(a[3]) || !none_or_tensor(a[6]) || s.L < 64 ||
+      !queries_of(a[1], a[4], a[5], s, &q))
+    Py_RETURN_NONE;
+  const int64_t T = s.L / 64, bound_sizes[5] = {s.B, s.Hkv, T, 2, s.D}, many[4] = {s.B, s.Hkv, q.n, T}, one[3] = {s.B, s.Hkv, T};
+  const at::IntArrayRef sizes = q.one ? at::IntArrayRef(one) : at::IntArrayRef(many);
+  if (!whole(tensor(a[2]), element_type(s), bound_sizes) || (a[3] != Py_None && !whole(tensor(a[3]), at::kInt, one)) ||
+      (a[6] != Py_None && !whole(tensor(a[6]), at::kFloat, sizes)))
+    Py_RETURN_NONE;
+  const void* bounds_ptr = address(a[2]);
+  const int32_t* map = (const int32_t*)address(a[3]);
+  void* out_ptr = address(a[6]);
+  const at::Tensor& like = tensor(a[1]);
+  at::Tensor out;
+  int rc;
+  {
+    NoGil others_run;
+    if (a[6] == Py_None) { out = NewTensors(like)(sizes, at::kFloat); out_ptr = out.data_ptr(); }
+    rc = g_hs.scores(&s, (int32_t)q.n, q.q_start, q.causal, &q.view, bounds_ptr, map, (float*)out_ptr, current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  return kept_or_made(a[6], out);
+  END_HANDLE_TH_ERRORS
+}
+
+// pick(shape, scores, n, first, last, out) -> out
+PyObject* pick(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  int32_t n, first, last;
+  if (n_args != 6 || !get_shape(a[0], &s) || !exact_tensor(a[1]) || !get_int(a[2], &n) || !get_int(a[3], &first) || !get_int(a[4], &last) ||
+      !none_or_tensor(a[5]) || n < 1 || s.L < 64)
+    Py_RETURN_NONE;
+  const at::Tensor& x = tensor(a[1]);
+  const bool flat = x.dim() == 3;
+  if ((!flat && x.dim() != 4) || x.scalar_type() != at::kFloat || !x.is_contiguous() || !here(x) || x.size(0) != s.B || x.size(1) != s.Hkv ||
+      x.size(x.dim() - 1) != s.L / 64)
+    Py_RETURN_NONE;
+  const int64_t Lq = flat ? 1 : x.size(2), many[4] = {s.B, s.Hkv, Lq, n}, one[3] = {s.B, s.Hkv, n};
+  const at::IntArrayRef sizes = flat ? at::IntArrayRef(one) : at::IntArrayRef(many);
+  if (Lq > INT32_MAX || (a[5] != Py_None && !whole(tensor(a[5]), at::kInt, sizes))) Py_RETURN_NONE;
+  const float* from = (const float*)x.data_ptr();
+  void* out_ptr = address(a[5]);
+  at::Tensor out;
+  int rc;
+  {
+    NoGil others_run;
+    if (a[5] == Py_None) { out = NewTensors(x)(sizes, at::kInt); out_ptr = out.data_ptr(); }
+    rc = g_hs.pick(&s, (int32_t)Lq, from, n, first, last, (int32_t*)out_ptr, current_stream());
+  }
+  if (rc != 0) return PyLong_FromLong(rc);
+  return kept_or_made(a[5], out);
+  END_HANDLE_TH_ERRORS
+}
+
+// listed(shape, Q, cache, tiles, causal, scale, q_start, tail_k, tail_v, tail_len, want_lse, out, lse, workspace) -> (out, lse)
+PyObject* listed(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  hs_shape s;
+  hs_kv kv;
+  Queries q;
+  float scale;
+  if (n_args != 14 || !get_shape(a[0], &s) || !exact_tensor(a[3]) || !get_float(a[5], &scale) || !PyBool_Check(a[10]) || s.L < 64) Py_RETURN_NONE;
+  for (int i : {7, 8, 11, 12, 13})
+    if (!none_or_tensor(a[i])) Py_RETURN_NONE;
+  if (!queries_of(a[1], a[4], a[6], s, &q) || !get_kv(a[2], &kv)) Py_RETURN_NONE;
+  bool ok;
+  if (!cache_here(a[2], &ok)) return nullptr;
+  if (!ok) Py_RETURN_NONE;
+  const at::Tensor& list = tensor(a[3]);
+  if (list.dim() < 3 || list.size(list.dim() - 1) > INT32_MAX) Py_RETURN_NONE;
+  const int64_t n = list.size(list.dim() - 1), many[4] = {s.B, s.Hkv, q.n, n}, one[3] = {s.B, s.Hkv, n};
+  if (!whole(list, at::kInt, q.one ? at::IntArrayRef(one) : at::IntArrayRef(many))) Py_RETURN_NONE;
+  const int64_t o_sizes[4] = {s.B, s.Hq, q.one ? s.D : q.n, s.D};
+  const at::IntArrayRef sizes(o_sizes, q.one ? 3 : 4), lse_sizes(o_sizes, q.one ? 2 : 3);
+  if ((a[11] != Py_None && !whole(tensor(a[11]), element_type(s), sizes)) || (a[12] != Py_None && !whole(tensor(a[12]), at::kFloat, lse_sizes)))
+    Py_RETURN_NONE;
+  const bool has_tail = a[7] != Py_None;
+  int32_t tail_len = 0;
+  const int32_t* lens = nullptr;
+  if (has_tail != (a[8] != Py_None) || has_tail != (a[9] != Py_None)) Py_RETURN_NONE;
+  if (has_tail) {
+    const int64_t tail_sizes[4] = {s.B, s.Hkv, 64, s.D};
+    if (!whole(tensor(a[7]), element_type(s), tail_sizes) || !whole(tensor(a[8]), element_type(s), tail_sizes) || !int_or_rows(a[9], {s.B}, &tail_len, &lens))
+      Py_RETURN_NONE;
+  }
+  size_t need = 0;
+  if (g_hs.listed_bytes(&s, (int32_t)q.n, (int32_t)n, has_tail, &need) != 0) Py_RETURN_NONE;
+  if (a[13] != Py_None && ((size_t)tensor(a[13]).nbytes() < need || !here(tensor(a[13])))) Py_RETURN_NONE;
+  const bool own_ws = a[13] == Py_None && need != 0, own_o = a[11] == Py_None, own_lse = a[12] == Py_None && a[10] == Py_True;
+  void *ws_ptr = address(a[13]), *o_ptr = address(a[11]);
+  float* lse_ptr = (float*)address(a[12]);
+  const int32_t* list_ptr = (const int32_t*)list.data_ptr();
+  const void *tk = address(a[7]), *tv = address(a[8]);
+  const at::Tensor& like = tensor(a[1]);
+  at::Tensor o, lse, ws;
+  int rc;
+  {
+    NoGil others_run;
+    if (own_ws || own_o || own_lse) {
+      const NewTensors make(like);
+      if (own_o) { o = make(sizes, like.scalar_type()); o_ptr = o.data_ptr(); }
+      if (own_lse) { lse = make(lse_sizes, at::kFloat); lse_ptr = (float*)lse.data_ptr(); }
+      if (own_ws) { ws = make.bytes(need); ws_ptr = ws.data_ptr(); }
+    }
+    rc = g_hs.listed(&s, (int32_t)q.n, q.q_start, scale, q.causal, &q.view, &kv, list_ptr, (int32_t)n, tk, tv, tail_len, lens, o_ptr, lse_ptr, ws_ptr,
+                     current_stream());
+  }
+  return result(rc, a[11], o, a[12], lse);
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses in the order of Entries, HsShape, HsPolicy, PackedKV, HsRope)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   constexpr Py_ssize_t n = sizeof(Entries) / sizeof(void*);
@@ -730,7 +920,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 
 #define HS_FN(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {HS_FN(bind), HS_FN(decode), HS_FN(decode_static), HS_FN(prefill), HS_FN(append), HS_FN(pools), HS_FN(compress), HS_FN(recompress),
-                          HS_FN(rope), HS_FN(mass), HS_FN(evict), HS_FN(keep),
+                          HS_FN(rope), HS_FN(mass), HS_FN(evict), HS_FN(keep), HS_FN(bounds), HS_FN(scores), HS_FN(pick), HS_FN(listed),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_hs_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
