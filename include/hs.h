@@ -488,7 +488,7 @@ HS_API int hs_tile_bounds(const hs_shape* shape, int32_t tile, int32_t n_tiles, 
  * (k_map: the cache's K map, device int32 [B, Hkv, L / 64], 0 = SKIP; NULL: no tile is), and causal those that begin behind the query.
  *   Q       [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i (0 <= q_start, q_start + Lq <= L if causal, else q_start is not looked at)
  *   scores  [B, Hkv, Lq, L / 64] contiguous
- * HS_EUNSUPPORTED beyond 2^24 - 1 workgroups of 64 tiles by (up to) 16 queries.  No workspace. */
+ * No workspace. */
 HS_API int hs_query_scores(const hs_shape* shape, int32_t Lq, int32_t q_start, int causal, const hs_view* Q, const void* bounds, const int32_t* k_map,
                     float* scores, void* stream);
 

@@ -808,7 +808,6 @@ int hs_query_scores(const hs_shape* shape, int32_t Lq, int32_t q_start, int caus
   a.bounds = (const uint16_t*)bounds; a.k_map = k_map; a.scores = scores;
   a.B = shape->B; a.Hq = shape->Hq; a.Hkv = shape->Hkv; a.T = shape->L / HS_BT;
   a.Lq = Lq; a.q_start = q_start; a.causal = causal != 0;
-  if (hs_scores_blocks(a) > HS_MAX_BLOCKS) return HS_EUNSUPPORTED;
   const hipError_t e = hs_launch_scores(a, shape->dtype, (hipStream_t)stream);
   return e != hipSuccess ? hip_fail(e) : HS_OK;
 }
@@ -829,7 +828,8 @@ int hs_listed_attn_workspace_bytes(const hs_shape* shape, int32_t Lq, int32_t n_
   const int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (Lq < 1 || n_list < 1 || bytes == nullptr) return HS_EINVAL;
-  *bytes = (size_t)hs_listed_parts(shape->B, shape->Hkv, Lq, n_list, with_tail != 0) * shape->B * shape->Hq * Lq * (HS_D + 1) * sizeof(float);
+  const int n = hs_listed_splits(shape->B, shape->Hkv, Lq, n_list);
+  *bytes = n > 1 ? (size_t)(n + (with_tail ? 1 : 0)) * shape->B * shape->Hq * Lq * (HS_D + 1) * sizeof(float) : 0;
   return HS_OK;
 }
 
@@ -859,9 +859,10 @@ int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float sca
   rc = view_of(Q, shape->B, shape->Hq, Lq, false, &a.q);
   if (rc != HS_OK) return rc;
   if (T > kSelectMaxTiles) return HS_EUNSUPPORTED;
-  const int64_t blocks = (int64_t)shape->B * shape->Hkv * ((int64_t)Lq * hs_listed_splits(shape->B, shape->Hkv, Lq, n_list) + 1);
+  const int n_splits = hs_listed_splits(shape->B, shape->Hkv, Lq, n_list);
+  const int64_t blocks = (int64_t)shape->B * shape->Hkv * ((int64_t)Lq * n_splits + 1);
   if (blocks > HS_MAX_BLOCKS / 2) return HS_EUNSUPPORTED;
-  if (hs_listed_parts(shape->B, shape->Hkv, Lq, n_list, tail_k != nullptr) > 0 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
+  if (n_splits > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;
   a.list = list;
   a.tail_k = (const uint16_t*)tail_k; a.tail_v = (const uint16_t*)tail_v; a.tail_lens = tail_lens;
   a.tail_len = tail_k == nullptr ? -1 : (tail_lens != nullptr ? 0 : tail_len);

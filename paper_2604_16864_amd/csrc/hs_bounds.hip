@@ -111,7 +111,6 @@ __global__ __launch_bounds__(64 * HS_BOUNDS_TILES) void bounds_kernel(hs_kv_dev 
 // sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c is a product over 256 terms: the bounds of 16 tiles are the A operand of the 16x16x32 matrix instruction
 // as they lie in memory, the positive and the negative parts of the queries the B operand.  Products of 16-bit numbers are exact in the
 // instruction, sums are held in 32 bits.
-// ONE: one query per sequence; columns are the group's heads, over again up to 16.  Else columns are 16 queries, one head after the other.
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : INFINITY; }  // a tile that cannot be ruled out
 
 __device__ __forceinline__ void parts_of(uint4 q, uint4& pos, uint4& neg) {
@@ -128,92 +127,124 @@ __device__ __forceinline__ void parts_of(uint4 q, uint4& pos, uint4& neg) {
 }
 
 template <bool F16>
-__device__ __forceinline__ f32x4_t bound_product(const uint4 (&low)[4], const uint4 (&high)[4], const uint16_t* q, int a) {
+__device__ __forceinline__ f32x4_t bound_product(const uint4 (&low)[4], const uint4 (&high)[4], const uint4 (&q)[4]) {
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-  uint4 v[4];
-#pragma unroll
-  for (int st = 0; st < 4; st++) v[st] = *reinterpret_cast<const uint4*>(q + 32 * st + 8 * a);
 #pragma unroll
   for (int st = 0; st < 4; st++) {
     uint4 pos, neg;
-    parts_of(v[st], pos, neg);
+    parts_of(q[st], pos, neg);
     s = hs_elem<F16>::mma(high[st], pos, s);
     s = hs_elem<F16>::mma(low[st], neg, s);
   }
   return s;
 }
+__device__ __forceinline__ void load_query(uint4 (&v)[4], const uint16_t* q, int a) {
+#pragma unroll
+  for (int st = 0; st < 4; st++) v[st] = *reinterpret_cast<const uint4*>(q + 32 * st + 8 * a);
+}
 
-template <bool F16, bool ONE>
-__global__ __launch_bounds__(256) void scores_kernel(hs_scores_args g, int64_t n_waves, int tile_blocks, int per_range) {
-  const int l = threadIdx.x & 63, a = l >> 4, c = l & 15, G = g.Hq / g.Hkv;
-  int64_t n = (int64_t)blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (n >= n_waves) return;
-  const int t0 = (int)(n % tile_blocks) * 16;
-  n /= tile_blocks;
-  const int row = (int)(n % ((int64_t)g.B * g.Hkv)), range = (int)(n / ((int64_t)g.B * g.Hkv));
-  const int b = row / g.Hkv, h = row - b * g.Hkv;
+// What of a row's 16 tiles from t0 on is needed: the bounds of tile t0 + l % 16, unless it is SKIP (m == 0).
+struct TileBounds {
   uint4 low[4], high[4];
-  const uint16_t* p = g.bounds + ((int64_t)row * g.T + min(t0 + c, g.T - 1)) * (2 * HS_D) + 8 * a;
+  __device__ __forceinline__ void load(const uint16_t* row, int t0, int m, int l) {
+    const uint16_t* p = row + (int64_t)(t0 + (l & 15)) * (2 * HS_D) + 8 * (l >> 4);
 #pragma unroll
-  for (int st = 0; st < 4; st++) {
-    low[st] = *reinterpret_cast<const uint4*>(p + 32 * st);
-    high[st] = *reinterpret_cast<const uint4*>(p + HS_D + 32 * st);
-  }
-  const int t = t0 + 4 * a, n_here = min(4, g.T - t);  // tiles of this lane's results
-  int held[4];
-#pragma unroll
-  for (int i = 0; i < 4; i++) held[i] = i < n_here ? (g.k_map != nullptr ? g.k_map[(int64_t)row * g.T + t + i] : 1) : 0;
-  const uint16_t* q = g.q.p + b * g.q.sb + (int64_t)h * G * g.q.sh;
-  const bool wide = (g.T & 3) == 0 && ((uintptr_t)g.scores & 15) == 0;
-  const int q_first = range * per_range, q_last = min(g.Lq, q_first + per_range);
-  for (int q0 = q_first; q0 < q_last; q0 += ONE ? 1 : 16) {
-    f32x4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    const int mine = ONE ? q0 : q0 + c;
-    if constexpr (ONE) {
-      best = bound_product<F16>(low, high, q + (c % G) * g.q.sh, a);
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        float x = no_nan(best[i]);
-#define HS_JOIN(CTRL_) x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL_, 0xf, 0xf, true)));
-        HS_JOIN(0x128) HS_JOIN(0x124) HS_JOIN(0x122) HS_JOIN(0x121)  // 8, 4, 2 and 1 lanes round the 16
-#undef HS_JOIN
-        best[i] = x;
-      }
-    } else {
-      for (int head = 0; head < G; head++) {
-        const f32x4_t s = bound_product<F16>(low, high, q + head * g.q.sh + min(mine, g.Lq - 1) * g.q.st, a);
-#pragma unroll
-        for (int i = 0; i < 4; i++) best[i] = fmaxf(best[i], no_nan(s[i]));
-      }
+    for (int st = 0; st < 4; st++) {
+      low[st] = m != 0 ? *reinterpret_cast<const uint4*>(p + 32 * st) : make_uint4(0, 0, 0, 0);
+      high[st] = m != 0 ? *reinterpret_cast<const uint4*>(p + HS_D + 32 * st) : make_uint4(0, 0, 0, 0);
     }
-    if (n_here <= 0 || (ONE ? c != 0 : mine >= q_last)) continue;
-    float* to = g.scores + ((int64_t)row * g.Lq + mine) * g.T + t;
-    float v[4];
+  }
+};
+
+// Four scores of one query, tiles t .. t + 3; held[i] == 0: SKIP, or behind the row.
+__device__ __forceinline__ void store_scores(const hs_scores_args& g, int row, int query, int t, f32x4_t s, const int (&held)[4], bool wide) {
+  float* to = g.scores + ((int64_t)row * g.Lq + query) * g.T + t;
+  float x[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) v[i] = held[i] != 0 && (!g.causal || (int64_t)(t + i) * HS_BT <= (int64_t)g.q_start + mine) ? best[i] : -INFINITY;
-    if (wide) {
-      *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
+  for (int i = 0; i < 4; i++) x[i] = held[i] != 0 && (!g.causal || (int64_t)(t + i) * HS_BT <= (int64_t)g.q_start + query) ? s[i] : -INFINITY;
+  if (wide) {
+    if (t < g.T) *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 4; i++)
-        if (i < n_here) to[i] = v[i];
+    for (int i = 0; i < 4; i++)
+      if (t + i < g.T) to[i] = x[i];
+  }
+}
+__device__ __forceinline__ bool wide_scores(const hs_scores_args& g) { return (g.T & 3) == 0 && ((uintptr_t)g.scores & 15) == 0; }
+
+// One query per sequence.  grid = (tiles, rows); a wave has n_blocks <= 4 blocks of 16 tiles, the next one requested while one is multiplied.  Columns are the
+// group's heads, over again up to 16.
+template <bool F16>
+__global__ __launch_bounds__(256) void scores_one_kernel(hs_scores_args g, int n_blocks) {
+  const int l = threadIdx.x & 63, a = l >> 4, c = l & 15, G = g.Hq / g.Hkv;
+  const int t0 = 16 * n_blocks * (int)(blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  if (t0 >= g.T) return;
+  const int row = blockIdx.y, b = row / g.Hkv, h = row - b * g.Hkv;
+  int m = l < 16 * n_blocks && t0 + l < g.T;  // whether tile t0 + l is held
+  if (g.k_map != nullptr && m != 0) m = g.k_map[(int64_t)row * g.T + t0 + l];
+  uint4 q[4];
+  load_query(q, g.q.p + b * g.q.sb + ((int64_t)h * G + c % G) * g.q.sh, a);
+  const uint16_t* bounds = g.bounds + (int64_t)row * g.T * (2 * HS_D);
+  const bool wide = wide_scores(g);
+  auto load = [&](TileBounds& r, int k) { r.load(bounds, t0 + 16 * k, __shfl(m, 16 * k + c), l); };
+  auto use = [&](const TileBounds& r, int k) {
+    f32x4_t s = bound_product<F16>(r.low, r.high, q);
+    int held[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      float x = no_nan(s[i]);
+#define HS_JOIN(CTRL_) x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL_, 0xf, 0xf, true)));
+      HS_JOIN(0x128) HS_JOIN(0x124) HS_JOIN(0x122) HS_JOIN(0x121)  // 8, 4, 2 and 1 lanes round the 16
+#undef HS_JOIN
+      s[i] = x;
+      held[i] = __shfl(m, 16 * k + 4 * a + i);
+    }
+    if (c == 0) store_scores(g, row, 0, t0 + 16 * k + 4 * a, s, held, wide);
+  };
+  TileBounds even, odd;
+  load(even, 0);
+  for (int k = 0; k < n_blocks; k += 2) {  // blocks behind the row have no held tile and are not stored
+    if (k + 1 < n_blocks) load(odd, k + 1);
+    use(even, k);
+    if (k + 1 < n_blocks) {
+      if (k + 2 < n_blocks) load(even, k + 2);
+      use(odd, k + 1);
     }
   }
 }
 
-struct ScoresPlan { int tile_blocks, per_range, threads; int64_t n_waves, blocks; };
-ScoresPlan plan_scores(const hs_scores_args& a) {
-  ScoresPlan p;
-  p.tile_blocks = (a.T + 15) / 16;
-  const int64_t fixed = (int64_t)p.tile_blocks * a.B * a.Hkv, blocks = ((int64_t)a.Lq + 15) / 16;
-  int64_t ranges = 2048 / fixed;
-  ranges = ranges < 1 ? 1 : (ranges > blocks ? blocks : ranges);
-  p.per_range = (int)((blocks + ranges - 1) / ranges) * 16;
-  ranges = ((int64_t)a.Lq + p.per_range - 1) / p.per_range;
-  p.n_waves = fixed * ranges;
-  p.threads = p.n_waves <= 1024 ? 64 : 256;
-  p.blocks = (p.n_waves + p.threads / 64 - 1) / (p.threads / 64);
-  return p;
+// More queries.  grid = (tiles, rows, ranges of the queries); a wave reads its 16 tiles once.  Columns are 16 queries, one head after the other, all heads'
+// queries requested at once.
+template <bool F16, int G>
+__global__ __launch_bounds__(256) void scores_kernel(hs_scores_args g, int per_range) {
+  const int l = threadIdx.x & 63, a = l >> 4, c = l & 15;
+  const int t0 = 16 * (int)(blockIdx.x * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  if (t0 >= g.T) return;
+  const int row = blockIdx.y, b = row / g.Hkv, h = row - b * g.Hkv;
+  const uint16_t* q = g.q.p + b * g.q.sb + (int64_t)h * G * g.q.sh;
+  int m = t0 + c < g.T;
+  if (g.k_map != nullptr && m != 0) m = g.k_map[(int64_t)row * g.T + t0 + c];
+  TileBounds r;
+  r.load(g.bounds + (int64_t)row * g.T * (2 * HS_D), t0, m, l);
+  int held[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) held[i] = __shfl(m, 4 * a + i);
+  const bool wide = wide_scores(g);
+  const int q_first = (int)blockIdx.z * per_range, q_last = min(g.Lq, q_first + per_range);
+  for (int q0 = q_first; q0 < q_last; q0 += 16) {
+    const uint16_t* from = q + min(q0 + c, q_last - 1) * g.q.st;
+    uint4 v[G][4];
+#pragma unroll
+    for (int k = 0; k < G; k++) load_query(v[k], from + k * g.q.sh, a);
+    f32x4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int k = 0; k < G; k++) {
+      const f32x4_t s = bound_product<F16>(r.low, r.high, v[k]);
+#pragma unroll
+      for (int i = 0; i < 4; i++) best[i] = fmaxf(best[i], no_nan(s[i]));
+    }
+    if (q0 + c < q_last) store_scores(g, row, q0 + c, t0 + 4 * a, best, held, wide);
+  }
 }
 
 }  // namespace
@@ -225,17 +256,31 @@ hipError_t hs_launch_bounds(int B, int Hkv, int T, const hs_kv_dev& kv, int tile
   return hipGetLastError();
 }
 
-int64_t hs_scores_blocks(const hs_scores_args& a) { return plan_scores(a).blocks; }
-
 hipError_t hs_launch_scores(const hs_scores_args& a, int dtype, hipStream_t st) {
-  const ScoresPlan p = plan_scores(a);
-#define HS_SCORES(F16_, ONE_) \
-  hipLaunchKernelGGL((scores_kernel<F16_, ONE_>), dim3((unsigned)p.blocks), dim3(p.threads), 0, st, a, p.n_waves, p.tile_blocks, p.per_range)
-  if (dtype == HS_FP16) {
-    if (a.Lq == 1) HS_SCORES(true, true); else HS_SCORES(true, false);
-  } else {
-    if (a.Lq == 1) HS_SCORES(false, true); else HS_SCORES(false, false);
+  const int rows = a.B * a.Hkv, tile_blocks = (a.T + 15) / 16;
+  const int64_t fixed = (int64_t)rows * tile_blocks;
+  if (a.Lq == 1) {
+    const int n = fixed >= 16384 ? 4 : (fixed >= 8192 ? 2 : 1);  // blocks of a wave
+    const int64_t per_row = (tile_blocks + n - 1) / n;
+    const int waves = per_row * rows <= 1024 ? 1 : 4;
+    const dim3 grid((unsigned)((per_row + waves - 1) / waves), (unsigned)rows), block(64 * waves);
+    if (dtype == HS_FP16) hipLaunchKernelGGL((scores_one_kernel<true>), grid, block, 0, st, a, n);
+    else hipLaunchKernelGGL((scores_one_kernel<false>), grid, block, 0, st, a, n);
+    return hipGetLastError();
   }
+  const int64_t blocks = ((int64_t)a.Lq + 15) / 16;
+  int64_t ranges = 2048 / fixed;
+  ranges = ranges < 1 ? 1 : (ranges > blocks ? blocks : ranges);
+  const int per_range = (int)((blocks + ranges - 1) / ranges) * 16;
+  ranges = ((int64_t)a.Lq + per_range - 1) / per_range;
+  const int waves = fixed * ranges <= 1024 ? 1 : 4;
+  const dim3 grid((unsigned)((tile_blocks + waves - 1) / waves), (unsigned)rows, (unsigned)ranges), block(64 * waves);
+#define HS_SCORES(G_)                                                                                    \
+  case G_:                                                                                               \
+    if (dtype == HS_FP16) hipLaunchKernelGGL((scores_kernel<true, G_>), grid, block, 0, st, a, per_range); \
+    else hipLaunchKernelGGL((scores_kernel<false, G_>), grid, block, 0, st, a, per_range);               \
+    break
+  switch (a.Hq / a.Hkv) { HS_SCORES(1); HS_SCORES(2); HS_SCORES(3); HS_SCORES(4); HS_SCORES(5); HS_SCORES(6); HS_SCORES(7); HS_SCORES(8); }
 #undef HS_SCORES
   return hipGetLastError();
 }

@@ -265,8 +265,6 @@ struct hs_scores_args {
   float* scores;
   int32_t B, Hq, Hkv, T, Lq, q_start, causal;
 };
-// workgroups of a call; at most HS_MAX_BLOCKS are launched
-int64_t hs_scores_blocks(const hs_scores_args& a);
 hipError_t hs_launch_scores(const hs_scores_args& a, int dtype, hipStream_t st);
 // rows of T <= 65536 scores, rows <= HS_MAX_BLOCKS / 4
 hipError_t hs_launch_pick(int64_t rows, int T, const float* scores, int n_pick, int first, int last, int32_t* list, hipStream_t st);
@@ -281,8 +279,10 @@ struct hs_listed_args {
   int32_t B, Hq, Hkv, T, Lq, q_start, causal, n_list, tail_len;  // tail_len < 0: no tail
   float scale;
 };
-// ranges that a query's list is cut into; with more than one (or one, and a tail that is a part of its own) the parts go through ws:
-// hs_listed_parts * B * Hq * Lq * 129 floats, 0 parts: none
+// shares that a query's list is cut into; with more than one their results go through ws: B * Hq * Lq * 129 floats for each, and as much for a tail
 int hs_listed_splits(int B, int Hkv, int Lq, int n_list);
-int hs_listed_parts(int B, int Hkv, int Lq, int n_list, int with_tail);
+struct hs_listed_plan { int splits, waves, stream; };  // waves of a workgroup: 4, or with stream 8; stream: tiles are read past the caches
 hipError_t hs_launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);
+// its kernels for tensors with both kinds of tile (km, vm: 0 all 2:4, 1 all dense, 2 mixed; one of them is 2); wo, wl: of the shares, or O and LSE
+hipError_t hs_launch_listed_mixed(int km, int vm, const hs_listed_args& a, const hs_kv_dev& kv, bool f16, hs_listed_plan p, float* wo, float* wl,
+                                  hipStream_t st);

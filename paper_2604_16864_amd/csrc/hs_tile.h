@@ -11,10 +11,14 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 
-// streaming (non-temporal) 16-byte load: the packed cache is read once per call
+// streaming (non-temporal) 16-byte load: decode attention reads the packed cache once per call
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
+}
+template <bool STREAM>
+__device__ __forceinline__ uint4 ld_tile(const uint4* p) {
+  if constexpr (STREAM) return ld_stream(p); else return *p;
 }
 
 
@@ -40,35 +44,38 @@ struct TileRegs {
   uint4 km, vm;  // the lane's four 32-bit index words of the K / V tile
 };
 
-template <int KM, int VM>
+// WHAT: 1 = K alone, 2 = V alone, 3 = both.  STREAM: what is read is not read again soon.
+template <int KM, int VM, int WHAT = 3, bool STREAM = true>
 __device__ __forceinline__ void tile_load(TileRegs<KM, VM>& r, const hs_kv_dev& kv, int64_t row, int mk, int mv, int l) {  // mk, mv: wave-uniform
   mv = hs_map_plain(mv);
-  r.km = make_uint4(0, 0, 0, 0);  // only 2:4 tiles carry index words
-  r.vm = make_uint4(0, 0, 0, 0);
+  if (WHAT & 1) r.km = make_uint4(0, 0, 0, 0);  // only 2:4 tiles carry index words
+  if (WHAT & 2) r.vm = make_uint4(0, 0, 0, 0);
   constexpr bool k_sparse = KM == 0, v_sparse = VM == 0;
-  if (k_sparse) {
+  if (!(WHAT & 1)) {
+  } else if (k_sparse) {
     const int64_t slot = row * kv.cap_sparse_k + (-mk - 1);
     const uint4* p = reinterpret_cast<const uint4*>(kv.k_nnz + slot * (int64_t)HS_TILE_NNZ_BYTES) + l;
 #pragma unroll
-    for (int i = 0; i < 8; i++) r.k[i] = ld_stream(p + 64 * i);
-    r.km = ld_stream(reinterpret_cast<const uint4*>(kv.k_meta + slot * (int64_t)HS_TILE_META_BYTES) + l);
+    for (int i = 0; i < 8; i++) r.k[i] = ld_tile<STREAM>(p + 64 * i);
+    r.km = ld_tile<STREAM>(reinterpret_cast<const uint4*>(kv.k_meta + slot * (int64_t)HS_TILE_META_BYTES) + l);
   } else {
     const int64_t slot = row * kv.cap_dense_k + (mk - 1);
     const uint4* p = reinterpret_cast<const uint4*>(kv.k_dense + slot * (int64_t)HS_TILE_DENSE_BYTES) + l;
 #pragma unroll
-    for (int i = 0; i < 16; i++) r.k[i % TileRegs<KM, VM>::kNK] = ld_stream(p + 64 * i);
+    for (int i = 0; i < 16; i++) r.k[i % TileRegs<KM, VM>::kNK] = ld_tile<STREAM>(p + 64 * i);
   }
-  if (v_sparse) {
+  if (!(WHAT & 2)) {
+  } else if (v_sparse) {
     const int64_t slot = row * kv.cap_sparse_v + (-mv - 1);
     const uint4* p = reinterpret_cast<const uint4*>(kv.v_nnz + slot * (int64_t)HS_TILE_NNZ_BYTES) + l;
 #pragma unroll
-    for (int i = 0; i < 8; i++) r.v[i] = ld_stream(p + 64 * i);
-    r.vm = ld_stream(reinterpret_cast<const uint4*>(kv.v_meta + slot * (int64_t)HS_TILE_META_BYTES) + l);
+    for (int i = 0; i < 8; i++) r.v[i] = ld_tile<STREAM>(p + 64 * i);
+    r.vm = ld_tile<STREAM>(reinterpret_cast<const uint4*>(kv.v_meta + slot * (int64_t)HS_TILE_META_BYTES) + l);
   } else {
     const int64_t slot = row * kv.cap_dense_v + (mv - 1);
     const uint4* p = reinterpret_cast<const uint4*>(kv.v_dense + slot * (int64_t)HS_TILE_DENSE_BYTES) + l;
 #pragma unroll
-    for (int i = 0; i < 16; i++) r.v[i % TileRegs<KM, VM>::kNV] = ld_stream(p + 64 * i);
+    for (int i = 0; i < 16; i++) r.v[i % TileRegs<KM, VM>::kNV] = ld_tile<STREAM>(p + 64 * i);
   }
 }
 
@@ -281,10 +288,10 @@ __device__ __forceinline__ void tail_piece(const TailArgs& tail, int tail_len, i
     }
   }
 }
-
 // Combines the N parts that the waves have left in LDS (and, with_tail, the tail's four behind them) and writes the row's partial of split
 // `slot`, or (DIRECT) its O and LSE.  hq0: the row of O of the group's first head, head_rows: rows from a head to the next.  Thread = (head tid / 32, 4 channels).  part_m, part_l, part_o: 8 heads a part.
-template <bool F16, bool DIRECT, int N>
+// TAIL: the dense tail's four parts may stand behind the N.
+template <bool F16, bool DIRECT, int N, bool TAIL = DIRECT>
 __device__ __forceinline__ void combine_parts(int tid, bool with_tail, int G, int64_t hq0, int64_t head_rows, const float (*part_m)[8], const float (*part_l)[8],
                                               const float (*part_o)[8][HS_D], int n_splits, int slot, float* __restrict__ ws_o,
                                               float* __restrict__ ws_l) {
@@ -294,7 +301,7 @@ __device__ __forceinline__ void combine_parts(int tid, bool with_tail, int G, in
   float mstar = -INFINITY;
 #pragma unroll
   for (int k = 0; k < N; k++) mstar = fmaxf(mstar, part_m[k][g]);
-  if (DIRECT && with_tail) {
+  if (TAIL && with_tail) {
 #pragma unroll
     for (int k = N; k < N + 4; k++) mstar = fmaxf(mstar, part_m[k][g]);
   }
@@ -310,7 +317,7 @@ __device__ __forceinline__ void combine_parts(int tid, bool with_tail, int G, in
   };
 #pragma unroll
   for (int k = 0; k < N; k++) add(k);
-  if (DIRECT && with_tail) {
+  if (TAIL && with_tail) {
 #pragma unroll
     for (int k = N; k < N + 4; k++) add(k);
   }
