@@ -507,9 +507,10 @@ HS_API int hs_pick_tiles(const hs_shape* shape, int32_t Lq, const float* scores,
  *         (tail_lens: device int32 [B] instead, clamped into 0 .. 64); it is attended to whatever the list says
  *   O     [B, Hq, Lq, D], LSE fp32 [B, Hq, Lq] or NULL, contiguous.  Nothing seen: O = 0, LSE = -inf; a score that is NaN: O = NaN, LSE = NaN.
  *         Keys and values that a query does not see do not touch its results, infinities and NaN among them.
- * scale as for hs_prefill_attn.  L / 64 <= 65536, B Hkv (Lq + 1) < 2^23 (HS_EUNSUPPORTED beyond).  workspace: hs_listed_attn_workspace_bytes
- * bytes, 16-byte aligned (NULL where that is 0), not shared between two calls in flight; no initial content.  Equal calls give equal bits, and so do lists
- * that name the same tiles with the same n_list. */
+ * scale as for hs_prefill_attn.  Of single queries the softmax numerators enter the second product in two 16-bit terms, as in decode attention; where many queries
+ * share the work, in one fp16 term or, for values that fp16 does not hold, two bf16 terms, as in prefill.  L / 64 <= 65536, n_list <= 2^20,
+ * B Hkv (Lq + 1) < 2^23 (HS_EUNSUPPORTED beyond).  workspace: hs_listed_attn_workspace_bytes bytes, 16-byte aligned (NULL where that is 0), not shared between two
+ * calls in flight; no initial content.  Equal calls give equal bits, and so do lists that name the same tiles with the same n_list. */
 HS_API int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q, const hs_kv* kv,
                    const int32_t* list, int32_t n_list, const void* tail_k, const void* tail_v, int32_t tail_len, const int32_t* tail_lens,
                    void* O, float* LSE, void* workspace, void* stream);

@@ -55,11 +55,11 @@ def pick_tiles(scores, n, first, last):
     return out.reshape(scores.shape[:-1] + (n,))
 
 
-def listed_attention(Q, K, V, lists, held, scale, positions=None, tail_k=None, tail_v=None, tail_lens=None):
+def listed_attention(Q, K, V, lists, held, scale, positions=None, tail_k=None, tail_v=None, tail_lens=None, weight=2.0 ** -16):
     """Q [B, Hq, Lq, D], K, V [B, Hkv, L, D] float64, lists int [B, Hkv, Lq, n].  Returns O, LSE and for each a bound on its error in the arithmetic of a
-    matrix product with 32-bit sums and weights of 16 bits or more: a score is a sum of D exact products, off by at most D steps of 2^-24 of the sum of their
-    magnitudes (twice that where sums are cut, not rounded); scale and exponent each by 2^-24 of the argument; an exponential by 2^-22; a weight is
-    held in two terms of 8 bits or more, off by 2^-16; each sum of n terms by n 2^-24, and by as much again where parts are joined."""
+    matrix product with 32-bit sums: a score is a sum of D exact products, off by at most D steps of 2^-24 of the sum of their
+    magnitudes (twice that where sums are cut, not rounded); scale and exponent each by 2^-24 of the argument; an exponential by 2^-22; a weight that
+    multiplies a value by `weight` (two terms of 8 bits or more: 2^-16; one of 11 bits: 2^-12); each sum of n terms by n 2^-24, and by as much again where parts are joined."""
     B, Hq, Lq, D = Q.shape
     H, T = K.shape[1], K.shape[2] // TILE
     G = Hq // H
@@ -85,6 +85,6 @@ def listed_attention(Q, K, V, lists, held, scale, positions=None, tail_k=None, t
                     O[b, g, i], LSE[b, g, i] = p @ v / p.sum(), m + np.log(p.sum())
                     off = scale * 2 * D * e * (np.abs(k) @ np.abs(q)).max() + 4 * e * np.abs(s).max() * 1.5
                     size = p @ np.abs(v) / p.sum()
-                    o_tol[b, g, i] = size * (2 * off + 2.0 ** -16 + 2.0 ** -21 + 4 * len(k) * e)
+                    o_tol[b, g, i] = size * (2 * off + weight + 2.0 ** -21 + 4 * len(k) * e)
                     l_tol[b, g, i] = off + 2.0 ** -21 + 4 * e * abs(LSE[b, g, i]) + 4 * len(k) * e
     return O, LSE, o_tol, l_tol

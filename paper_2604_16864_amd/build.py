@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhs.so")
 NATIVE = os.path.join(HERE, "_hs_torch.so")
 SOURCES = ["hs_api.hip", "hs_compress.hip", "hs_decode.hip", "hs_prefill.hip", "hs_prefill_mixed.hip", "hs_prefill_narrow.hip", "hs_prefill_narrow_mixed.hip", "hs_probe.hip",
-           "hs_rope.hip", "hs_mass.hip", "hs_evict.hip", "hs_keep.hip", "hs_bounds.hip", "hs_pick.hip", "hs_listed.hip", "hs_listed_mixed.hip"]
+           "hs_rope.hip", "hs_mass.hip", "hs_evict.hip", "hs_keep.hip", "hs_bounds.hip", "hs_pick.hip", "hs_listed.hip", "hs_listed_mixed.hip", "hs_listed_many.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -828,7 +828,8 @@ int hs_listed_attn_workspace_bytes(const hs_shape* shape, int32_t Lq, int32_t n_
   const int rc = check_shape(shape);
   if (rc != HS_OK) return rc;
   if (Lq < 1 || n_list < 1 || bytes == nullptr) return HS_EINVAL;
-  const int n = hs_listed_splits(shape->B, shape->Hkv, Lq, n_list);
+  if (Lq > 1 << 30 || n_list > 1 << 20 || shape->L / HS_BT > kSelectMaxTiles) return HS_EUNSUPPORTED;
+  const int n = hs_plan_listed(shape->B, shape->Hq, shape->Hkv, shape->L / HS_BT, Lq, n_list).splits;
   *bytes = n > 1 ? (size_t)(n + (with_tail ? 1 : 0)) * shape->B * shape->Hq * Lq * (HS_D + 1) * sizeof(float) : 0;
   return HS_OK;
 }
@@ -858,8 +859,8 @@ int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float sca
   hs_listed_args a = {};
   rc = view_of(Q, shape->B, shape->Hq, Lq, false, &a.q);
   if (rc != HS_OK) return rc;
-  if (T > kSelectMaxTiles) return HS_EUNSUPPORTED;
-  const int n_splits = hs_listed_splits(shape->B, shape->Hkv, Lq, n_list);
+  if (T > kSelectMaxTiles || n_list > 1 << 20) return HS_EUNSUPPORTED;
+  const int n_splits = hs_plan_listed(shape->B, shape->Hq, shape->Hkv, T, Lq, n_list).splits;
   const int64_t blocks = (int64_t)shape->B * shape->Hkv * ((int64_t)Lq * n_splits + 1);
   if (blocks > HS_MAX_BLOCKS / 2) return HS_EUNSUPPORTED;
   if (n_splits > 1 && (workspace == nullptr || ((uintptr_t)workspace & 15u))) return HS_EINVAL;

@@ -279,10 +279,13 @@ struct hs_listed_args {
   int32_t B, Hq, Hkv, T, Lq, q_start, causal, n_list, tail_len;  // tail_len < 0: no tail
   float scale;
 };
-// shares that a query's list is cut into; with more than one their results go through ws: B * Hq * Lq * 129 floats for each, and as much for a tail
-int hs_listed_splits(int B, int Hkv, int Lq, int n_list);
-struct hs_listed_plan { int splits, waves, stream; };  // waves of a workgroup: 4, or with stream 8; stream: tiles are read past the caches
+// shares that a list is cut into, waves of a workgroup (4, or 8 for single queries in one share), and neighbouring queries of a workgroup; with more than one share
+// their results go through ws: B * Hq * Lq * 129 floats for each, and as much for a tail.  Workgroups: B Hkv ceil(Lq / queries) splits.
+struct hs_listed_plan { int splits, waves, queries; };
+hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list);
 hipError_t hs_launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, int dtype, hipStream_t st);
 // its kernels for tensors with both kinds of tile (km, vm: 0 all 2:4, 1 all dense, 2 mixed; one of them is 2); wo, wl: of the shares, or O and LSE
 hipError_t hs_launch_listed_mixed(int km, int vm, const hs_listed_args& a, const hs_kv_dev& kv, bool f16, hs_listed_plan p, float* wo, float* wl,
                                   hipStream_t st);
+// for neighbouring queries that share workgroups (queries > 1), tensors of any kinds
+hipError_t hs_launch_listed_many(int km, int vm, const hs_listed_args& a, const hs_kv_dev& kv, bool f16, hs_listed_plan p, float* wo, float* wl, hipStream_t st);

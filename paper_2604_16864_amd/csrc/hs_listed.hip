@@ -11,18 +11,25 @@
 // of 8 waves while every one has a compute unit to itself.  The shares do not depend on the tiles' kinds: the workspace's size follows from them.
 // A step of single tokens reads past the caches: what it reads comes again with the next step, when the other layers' have gone through them.  128 rows of 64 tiles, 151 MB
 // that are not in the last-level cache: 30.7 us, through the caches 34.9; 512 rows 94 and 108.  Queries that stand side by side pick much the same tiles, and
-// read through the caches: 65 of them with 41 tiles each on 4 rows 21.2 us, past them 29.9.
-int hs_listed_splits(int B, int Hkv, int Lq, int n_list) {
-  const int64_t rows = (int64_t)B * Hkv * Lq;
-  if (rows > 128 || n_list <= 8 || (rows > 64 && n_list <= 32)) return 1;
-  const int by_rows = (int)(256 / rows), by_tiles = n_list / 4 + (n_list % 4 != 0);
-  return by_rows < by_tiles ? by_rows : by_tiles;
-}
-static hs_listed_plan plan(const hs_listed_args& a) {
-  hs_listed_plan p;
-  p.splits = hs_listed_splits(a.B, a.Hkv, a.Lq, a.n_list);
-  p.stream = a.Lq == 1;
-  p.waves = p.splits == 1 && (int64_t)a.B * a.Hkv <= 256 && p.stream ? 8 : 4;
+// read through the caches: 65 of them with 41 tiles each on 4 rows 22.2 us, past them 29.9.
+// Neighbouring queries in one workgroup, over all tiles that one of them picks (hs_listed_many.hip), against one by one, lists that differ in a third of their tiles:
+// 32 rows 11.9 and 9.9, 128 rows 15.3 and 13.9, 256 rows 19.2 and 20.4, 320 rows 15.2 and 16.1 (dense 18.4 and 22.4; 8 heads a row, two queries a workgroup, 17.8 and
+// 16.7), 384 rows 20.6 and 25.9, 600 rows 25.7 and 38.6, 2400 rows 56.5 and 111.
+hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list) {
+  hs_listed_plan p{1, 4, 1};
+  int64_t rows = (int64_t)B * Hkv * Lq;
+  if (Lq > 1 && rows > 300) {
+    // as many neighbours as columns and 24 KB of bit maps hold
+    const int columns = 16 / (Hq / Hkv), maps = 6144 / ((T + 31) / 32);
+    p.queries = columns < maps ? columns : maps;
+    if (p.queries > Lq) p.queries = Lq;
+    rows = (int64_t)B * Hkv * (((int64_t)Lq + p.queries - 1) / p.queries);
+  } else if (rows > 128 || n_list <= 8 || (rows > 64 && n_list <= 32)) {
+    if (rows <= 256 && Lq == 1) p.waves = 8;
+    return p;
+  }
+  const int by_rows = rows > 256 ? 1 : (int)(256 / rows), by_tiles = n_list / 4 + (n_list % 4 != 0);
+  p.splits = by_rows < by_tiles ? by_rows : by_tiles;
   return p;
 }
 
@@ -30,7 +37,7 @@ hipError_t hs_launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, int dt
   const int km = kv.cap_dense_k == 0 ? 0 : (kv.cap_sparse_k == 0 ? 1 : 2);
   const int vm = kv.cap_dense_v == 0 ? 0 : (kv.cap_sparse_v == 0 ? 1 : 2);
   const bool f16 = dtype == HS_FP16;
-  const hs_listed_plan p = plan(a);
+  const hs_listed_plan p = hs_plan_listed(a.B, a.Hq, a.Hkv, a.T, a.Lq, a.n_list);
   const bool direct = p.splits == 1;
   const int n_parts = p.splits + (a.tail_len >= 0 ? 1 : 0);
   const int64_t rows = (int64_t)a.B * a.Hq * a.Lq;
@@ -39,7 +46,8 @@ hipError_t hs_launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, int dt
   hipError_t e = hipSuccess;
 #define HS_GO(KM_, VM_) \
   e = kv.uniform ? launch_listed<KM_, VM_, true>(a, kv, f16, p, wo, wl, st) : launch_listed<KM_, VM_, false>(a, kv, f16, p, wo, wl, st)
-  if (km == 2 || vm == 2) e = hs_launch_listed_mixed(km, vm, a, kv, f16, p, wo, wl, st);
+  if (p.queries > 1) e = hs_launch_listed_many(km, vm, a, kv, f16, p, wo, wl, st);
+  else if (km == 2 || vm == 2) e = hs_launch_listed_mixed(km, vm, a, kv, f16, p, wo, wl, st);
   else if (km == 0 && vm == 0) HS_GO(0, 0);
   else if (km == 0) HS_GO(0, 1);
   else if (vm == 0) HS_GO(1, 0);

@@ -1,6 +1,7 @@
 // Attention of every query over the tiles that its list names: decode attention's work on a tile, with tiles handed out from a list.
 // Included by the translation units that instantiate it: hs_listed.hip (tensors of one kind) and hs_listed_mixed.hip.
 #pragma once
+#include "hs_rank.h"
 #include "hs_tile.h"
 
 namespace {
@@ -125,12 +126,7 @@ void listed_kernel(hs_listed_args g, hs_kv_dev kv, int n_splits, float scale_log
     w1 = min(n_words, w0 + per);
     int mine = 0;
     for (int i = w0; i < w1; i++) mine += __builtin_popcount(sm_bits[i]);
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int below = __shfl_up(upto, d);
-      if (l >= d) upto += below;
-    }
+    const int upto = wave_upto(mine);
     if (l == 63) sm_cnt[w] = upto;
     __syncthreads();
     first = upto - mine;
@@ -295,16 +291,19 @@ void listed_kernel(hs_listed_args g, hs_kv_dev kv, int n_splits, float scale_log
 
 template <int KM, int VM, bool UNIFORM>
 hipError_t launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, bool f16, hs_listed_plan p, float* wo, float* wl, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * (a.Lq * p.splits + (p.splits > 1 && a.tail_len >= 0 ? 1 : 0)))), block(64 * p.waves);
+  const dim3 grid((unsigned)((int64_t)a.B * a.Hkv * ((int64_t)a.Lq * p.splits + (p.splits > 1 && a.tail_len >= 0 ? 1 : 0)))), block(64 * p.waves);
   const size_t lds = (size_t)(a.T + 31) / 32 * 4;
   const float sl2 = a.scale * kLog2e;
 #define HS_LISTED(F16_, NW_, STREAM_) \
   hipLaunchKernelGGL((listed_kernel<KM, VM, F16_, UNIFORM, NW_, STREAM_>), grid, block, lds, st, a, kv, p.splits, sl2, wo, wl)
+#define HS_LISTED_AS(F16_) \
+  if (a.Lq > 1) HS_LISTED(F16_, 4, false); else if (p.waves == 8) HS_LISTED(F16_, 8, true); else HS_LISTED(F16_, 4, true)
   if (f16) {
-    if (p.waves == 8) HS_LISTED(true, 8, true); else if (p.stream) HS_LISTED(true, 4, true); else HS_LISTED(true, 4, false);
+    HS_LISTED_AS(true);
   } else {
-    if (p.waves == 8) HS_LISTED(false, 8, true); else if (p.stream) HS_LISTED(false, 4, true); else HS_LISTED(false, 4, false);
+    HS_LISTED_AS(false);
   }
+#undef HS_LISTED_AS
 #undef HS_LISTED
   return hipGetLastError();
 }

@@ -255,7 +255,7 @@ def test_listed_attention(B, G, Hkv, T, Lq, n, policy, dtype):
     first = T * TILE - Lq
     for causal, at, scale in ((False, None, 0.0), (True, None, 0.0), (True, first // 2, 0.02)):
         pos = (first if at is None else at) + np.arange(Lq) if causal else None
-        want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, scale or D ** -0.5, pos)
+        want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, scale or D ** -0.5, pos, weight=2.0 ** (-16 if Lq == 1 else -12))
         o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=causal, q_start=at, scale=scale)
         _close_attention(o, lse, want, TYPES[dtype], (causal, at))
     if Lq == 1:
@@ -327,12 +327,61 @@ def test_unseen_tokens_do_not_touch_results(bad, policy, dtype):
     at = 4 * TILE + 21 - Lq
     o, lse = hb.listed_attn(sh, Q.cuda(), dirty, lists.cuda(), q_start=at)
     want = ref.listed_attention(_f64(Q), np.nan_to_num(_f64(K), nan=0.0, posinf=0.0, neginf=0.0), np.nan_to_num(_f64(V), nan=0.0, posinf=0.0, neginf=0.0), lists.numpy(), held,
-                                D ** -0.5, at + np.arange(Lq))
+                                D ** -0.5, at + np.arange(Lq), weight=2.0 ** -12)
     _close_attention(o, lse, want, TYPES[dtype])
     # a query that sees one: NaN, or what infinities give
     o, lse = hb.listed_attn(sh, Q[:, :, :1].cuda(), dirty, lists[:, :, :1].contiguous().cuda(), q_start=4 * TILE + 21)
     if math.isnan(bad) and bool(held[0, 0, 4]):
         assert bool(torch.isnan(o[0, :2]).all()) and bool(torch.isnan(lse[0, :2]).all())
+
+
+@gpu
+@pytest.mark.parametrize("G", [1, 2, 3, 7])
+@pytest.mark.parametrize("policy", ["2:4", "dense", "half"])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_tiles_of_neighbouring_queries_do_not_touch_results(bad, policy, G):
+    """Queries that do not list a tile whose keys and values are no numbers, between others that do."""
+    T, Lq, Hkv = 7, 37, 2
+
+    def spoil(K, V):
+        K[:, 0, 2 * TILE:3 * TILE] = bad
+        V[:, :, 2 * TILE + 5:3 * TILE:4] = bad
+    _, clean, _, _, _ = _cache(1, G * Hkv, Hkv, T, "bf16", policy, 6)
+    states = [torch.where(m > 0, hb.DENSE, hb.SPARSE24).to(torch.int8) for m in (clean.k_map, clean.v_map)]
+    sh, kv, K, V, held = _cache(1, G * Hkv, Hkv, T, "bf16", hb.make_policy(state_k=states[0], state_v=states[1]), 6, spoil)
+    Q = torch.randn((1, G * Hkv, Lq, D), generator=_gen(1)).bfloat16()
+    lists = torch.full((1, Hkv, Lq, 4), -1, dtype=torch.int32)
+    lists[..., :3] = torch.tensor([6, 0, 3])
+    lists[:, :, ::3, 3] = 2
+    o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=False)
+    zero = [np.nan_to_num(_f64(x), nan=0.0, posinf=0.0, neginf=0.0) for x in (K, V)]
+    want = ref.listed_attention(_f64(Q), *zero, np.where(lists.numpy() == 2, -1, lists.numpy()), held, D ** -0.5, weight=2.0 ** -12)
+    rest = np.arange(Lq) % 3 != 0
+    _close_attention(o[:, :, rest], lse[:, :, rest], tuple(x[:, :, rest] for x in want), torch.bfloat16)
+    assert not bool(torch.isfinite(o[:, :, ::3].float()).all(-1).any())
+
+
+@gpu
+@pytest.mark.parametrize("T,n", [(3000, 40), (9000, 9), (65536, 5)])
+def test_many_queries_on_long_rows(T, n):
+    """Rows of more tiles than the bit maps of 16 queries hold: against single queries, whose lists they are."""
+    Lq = 21
+    sh = hb.make_shape(1, 2, 1, T * TILE)
+    small = hb.make_shape(1, 2, 1, 8 * TILE)
+    K = torch.randn((1, 1, 8 * TILE, D), generator=_gen(3)).bfloat16().cuda()
+    few = hb.compress_kv(small, hb.make_policy(), K, K)
+    kv = hb.PackedKV(sh, [T - 8, 0, 8, 0, 8], "cuda")          # slots that repeat: a valid cache to read
+    kv.k_nnz, kv.k_meta, kv.v_nnz, kv.v_meta = few.k_nnz, few.k_meta, few.v_nnz, few.v_meta
+    slots = -(torch.arange(T, dtype=torch.int32, device="cuda") % 8 + 1)
+    kv.k_map, kv.v_map = slots.repeat(1, 1, 1), slots.repeat(1, 1, 1) - (few.v_map[0, 0, 0].abs() & hb.MAP_F16)
+    Q = torch.randn((1, 2, Lq, D), generator=_gen(4)).bfloat16().cuda()
+    lists = torch.randint(0, T, (1, 1, Lq, n), generator=_gen(5), dtype=torch.int32).cuda()
+    lists[..., 0] = T - 1
+    o, lse = hb.listed_attn(sh, Q, kv, lists, causal=False)
+    for i in range(Lq):
+        o1, lse1 = hb.listed_attn(sh, Q[:, :, i], kv, lists[:, :, i].contiguous())
+        assert (o[:, :, i].float() - o1.float()).abs().max().item() <= 4 * 2.0 ** -8 * o1.float().abs().max().item(), i
+        assert (lse[:, :, i] - lse1).abs().max().item() <= 1e-4, i
 
 
 @gpu
@@ -590,15 +639,16 @@ def test_refusals_on_the_host():
                     (dict(lists=None), -1), (dict(lists=4098), -1), (dict(n=0), -1), (dict(o=None), -1), (dict(o=4097), -1), (dict(lse=4098), -1), (dict(tk=4096), -1),
                     (dict(tv=4096), -1), (dict(tk=4096, tv=4096), -2), (dict(one, tk=4096, tv=4096, tail_len=65), -1), (dict(one, tk=4096, tv=4096, tail_len=-1), -1),
                     (dict(one, tk=4104, tv=4096), -1), (dict(one, ws=None, n=64), -1), (dict(one, ws=4104, n=64), -1), (dict(cache=C.byref(uniform)), -1), (dict(shape=big), -2),
-                    (dict(Lq=(1 << 30) + 1, causal=0), -2), (dict(Lq=1 << 22, causal=0), -2), (dict(Q=view(token=4)), -1)):
+                    (dict(Lq=(1 << 30) + 1, causal=0), -2), (dict(Lq=1 << 22, causal=0), -2), (dict(n=(1 << 20) + 1), -2), (dict(Q=view(token=4)), -1)):
         assert listed(**bad) == rc, bad
     size = C.c_size_t(0)
     for bad in ((0, 4, C.byref(size)), (1, 0, C.byref(size)), (1, 4, None)):
         assert L.hs_listed_attn_workspace_bytes(s, bad[0], bad[1], 0, bad[2]) == -1
     assert hb.listed_attn_workspace_bytes(hb.make_shape(64, 32, 8, 65536), 1, 64, True) == 0
-    for n in (1, 5, 1 << 20, 2 ** 31 - 1):
-        for Lq in (1, 2, 100):
-            assert 0 <= hb.listed_attn_workspace_bytes(sh, Lq, n) <= 64 << 20
+    assert L.hs_listed_attn_workspace_bytes(s, 1, (1 << 20) + 1, 0, C.byref(size)) == -2 and L.hs_listed_attn_workspace_bytes(big, 1, 4, 0, C.byref(size)) == -2
+    for n in (1, 5, 1 << 20):
+        for Lq in (1, 2, 100, 5000):
+            assert 0 <= hb.listed_attn_workspace_bytes(sh, Lq, n) <= 16 << 20
 
 
 def test_refusals_of_the_binding():
