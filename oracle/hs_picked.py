@@ -59,7 +59,7 @@ def listed_attention(Q, K, V, lists, held, scale, positions=None, tail_k=None, t
     """Q [B, Hq, Lq, D], K, V [B, Hkv, L, D] float64, lists int [B, Hkv, Lq, n].  Returns O, LSE and for each a bound on its error in the arithmetic of a
     matrix product with 32-bit sums: a score is a sum of D exact products, off by at most D steps of 2^-24 of the sum of their
     magnitudes (twice that where sums are cut, not rounded); scale and exponent each by 2^-24 of the argument; an exponential by 2^-22; a weight that
-    multiplies a value by `weight` (two terms of 8 bits or more: 2^-16; one of 11 bits: 2^-12); each sum of n terms by n 2^-24, and by as much again where parts are joined."""
+    multiplies a value by `weight` (two terms of 8 bits or more: 2^-16; one of 11 bits, half a step of fp16: 2^-11); each sum of n terms by n 2^-24, and by as much again where parts are joined."""
     B, Hq, Lq, D = Q.shape
     H, T = K.shape[1], K.shape[2] // TILE
     G = Hq // H

@@ -203,6 +203,18 @@ def test_pick(T, Lq):
 
 
 @gpu
+@pytest.mark.parametrize("T", [90, 300, 700, 1500, 3000])
+def test_pick_for_many_queries(T):
+    """More than 512 rows, which other numbers of threads take."""
+    g = _gen(T)
+    sh = hb.make_shape(1, 3, 3, T * TILE)
+    s = (torch.randn((1, 3, 190, T), generator=g) * 4).half().float()
+    s[torch.rand(s.shape, generator=g) < 0.2] = -math.inf
+    for n, first, last in ((24, 1, 4), (1, 0, 0), (T // 2, 3, 0)):
+        assert (hb.pick_tiles(sh, s.cuda(), n, first, last).cpu().numpy() == ref.pick_tiles(s.numpy(), n, first, last)).all(), (n, first, last)
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["alike", "two values", "zeros of both signs", "special", "none", "near"])
 @pytest.mark.parametrize("T", [100, 1000, 5000, 20000])
 def test_pick_of_special_scores(T, kind):
@@ -247,15 +259,17 @@ def _close_attention(got_o, got_lse, want, dtype, what=""):
 @gpu
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("policy", sorted(POLICIES))
-@pytest.mark.parametrize("B,G,Hkv,T,Lq,n", [(1, 1, 1, 1, 1, 1), (2, 4, 2, 9, 1, 5), (1, 8, 1, 40, 1, 70), (1, 7, 2, 12, 5, 6), (2, 3, 2, 6, 70, 3)])
+@pytest.mark.parametrize("B,G,Hkv,T,Lq,n", [(1, 1, 1, 1, 1, 1), (2, 4, 2, 9, 1, 5), (1, 8, 1, 40, 1, 70), (1, 7, 2, 12, 5, 6), (2, 3, 2, 6, 70, 3), (1, 2, 4, 33, 2, 20),
+                                            (1, 5, 1, 8, 301, 4), (2, 1, 2, 7, 90, 30)])
 def test_listed_attention(B, G, Hkv, T, Lq, n, policy, dtype):
     sh, kv, K, V, held = _cache(B, G * Hkv, Hkv, T, dtype, policy, 7 * T + n)
     Q = torch.randn((B, G * Hkv, Lq, D), generator=_gen(n)).to(TYPES[dtype])
     lists = _lists(B, Hkv, Lq, T, n, 3 * n)
+    lists[:, :, Lq // 2 + 1:Lq // 2 + 3] = -1          # queries with no tile at all
     first = T * TILE - Lq
     for causal, at, scale in ((False, None, 0.0), (True, None, 0.0), (True, first // 2, 0.02)):
         pos = (first if at is None else at) + np.arange(Lq) if causal else None
-        want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, scale or D ** -0.5, pos, weight=2.0 ** (-16 if Lq == 1 else -12))
+        want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, scale or D ** -0.5, pos, weight=2.0 ** (-16 if B * Hkv * Lq <= 300 else -11))
         o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=causal, q_start=at, scale=scale)
         _close_attention(o, lse, want, TYPES[dtype], (causal, at))
     if Lq == 1:
@@ -310,10 +324,12 @@ def test_lists_are_sets(policy, dtype):
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("policy", ["2:4", "dense", "dense keys", "dense values", "some of half"])
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
-def test_unseen_tokens_do_not_touch_results(bad, policy, dtype):
-    """Keys and values that are no numbers: in tiles that are not listed, and behind a causal query within its tile."""
-    T, Lq = 6, 130
-    sh, clean, _, _, _ = _cache(1, 4, 2, T, dtype, policy if policy == "some of half" else policy, 6)
+@pytest.mark.parametrize("Lq", [130, 170])
+def test_unseen_tokens_do_not_touch_results(Lq, bad, policy, dtype):
+    """Keys and values that are no numbers: in tiles that are not listed, and behind a causal query within its tile.  Queries by themselves, and in
+    company (more than 300 of them)."""
+    T = 6
+    sh, clean, _, _, _ = _cache(1, 4, 2, T, dtype, policy, 6)
     states = [torch.where(m == 0, hb.SKIP, torch.where(m > 0, hb.DENSE, hb.SPARSE24)).to(torch.int8) for m in (clean.k_map, clean.v_map)]
 
     def spoil(K, V):
@@ -327,7 +343,7 @@ def test_unseen_tokens_do_not_touch_results(bad, policy, dtype):
     at = 4 * TILE + 21 - Lq
     o, lse = hb.listed_attn(sh, Q.cuda(), dirty, lists.cuda(), q_start=at)
     want = ref.listed_attention(_f64(Q), np.nan_to_num(_f64(K), nan=0.0, posinf=0.0, neginf=0.0), np.nan_to_num(_f64(V), nan=0.0, posinf=0.0, neginf=0.0), lists.numpy(), held,
-                                D ** -0.5, at + np.arange(Lq), weight=2.0 ** -12)
+                                D ** -0.5, at + np.arange(Lq), weight=2.0 ** (-16 if 2 * Lq <= 300 else -11))
     _close_attention(o, lse, want, TYPES[dtype])
     # a query that sees one: NaN, or what infinities give
     o, lse = hb.listed_attn(sh, Q[:, :, :1].cuda(), dirty, lists[:, :, :1].contiguous().cuda(), q_start=4 * TILE + 21)
@@ -341,7 +357,7 @@ def test_unseen_tokens_do_not_touch_results(bad, policy, dtype):
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_tiles_of_neighbouring_queries_do_not_touch_results(bad, policy, G):
     """Queries that do not list a tile whose keys and values are no numbers, between others that do."""
-    T, Lq, Hkv = 7, 37, 2
+    T, Lq, Hkv = 7, 160, 2
 
     def spoil(K, V):
         K[:, 0, 2 * TILE:3 * TILE] = bad
@@ -355,7 +371,7 @@ def test_tiles_of_neighbouring_queries_do_not_touch_results(bad, policy, G):
     lists[:, :, ::3, 3] = 2
     o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=False)
     zero = [np.nan_to_num(_f64(x), nan=0.0, posinf=0.0, neginf=0.0) for x in (K, V)]
-    want = ref.listed_attention(_f64(Q), *zero, np.where(lists.numpy() == 2, -1, lists.numpy()), held, D ** -0.5, weight=2.0 ** -12)
+    want = ref.listed_attention(_f64(Q), *zero, np.where(lists.numpy() == 2, -1, lists.numpy()), held, D ** -0.5, weight=2.0 ** -11)
     rest = np.arange(Lq) % 3 != 0
     _close_attention(o[:, :, rest], lse[:, :, rest], tuple(x[:, :, rest] for x in want), torch.bfloat16)
     assert not bool(torch.isfinite(o[:, :, ::3].float()).all(-1).any())
@@ -365,7 +381,7 @@ def test_tiles_of_neighbouring_queries_do_not_touch_results(bad, policy, G):
 @pytest.mark.parametrize("T,n", [(3000, 40), (9000, 9), (65536, 5)])
 def test_many_queries_on_long_rows(T, n):
     """Rows of more tiles than the bit maps of 16 queries hold: against single queries, whose lists they are."""
-    Lq = 21
+    Lq = 310
     sh = hb.make_shape(1, 2, 1, T * TILE)
     small = hb.make_shape(1, 2, 1, 8 * TILE)
     K = torch.randn((1, 1, 8 * TILE, D), generator=_gen(3)).bfloat16().cuda()
@@ -419,6 +435,56 @@ def test_lists_longer_than_a_pass(n_tiles):
     a, b = hb.listed_attn(sh, Q, kv, every), hb.decode_attn(sh, Q, kv)
     assert (a[0].float() - b[0].float()).abs().max().item() <= 4 * 2.0 ** -11 * b[0].float().abs().max().item()
     assert (a[1] - b[1]).abs().max().item() <= 1e-4
+
+
+def _repeated(sh, small, T):
+    """A cache of T tiles a row whose slots are those of a small one, over and over: a valid cache to read."""
+    kv = hb.PackedKV(sh, [T - 4, 0, 4, 0, 4], "cuda")
+    kv.k_nnz, kv.k_meta, kv.v_nnz, kv.v_meta = small.k_nnz, small.k_meta, small.v_nnz, small.v_meta
+    at = torch.arange(T, dtype=torch.int32, device="cuda") % 4
+    kv.k_map, kv.v_map = (m[:, :, :1].repeat(1, 1, T) - at for m in (small.k_map, small.v_map))
+    return kv
+
+
+@gpu
+def test_bounds_and_scores_beyond_32_bits():
+    """Bounds of more than 4 GiB: the last rows of tiles against those that they repeat."""
+    B, Hkv, T = 20, 8, 60000
+    sh = hb.make_shape(B, Hkv, Hkv, T * TILE)
+    K = torch.randn((B, Hkv, 4 * TILE, D), generator=_gen(1)).bfloat16().cuda()
+    few_shape = hb.make_shape(B, Hkv, Hkv, 4 * TILE)
+    few = hb.compress_kv(few_shape, hb.make_policy(), K, K)
+    kv = _repeated(sh, few, T)
+    bounds, small = hb.tile_bounds(sh, kv), hb.tile_bounds(few_shape, few)
+    assert bounds.numel() * 2 > 1 << 32
+    for t in (0, 1, 30000, T - 1):
+        assert torch.equal(_bits(bounds[:, :, t]), _bits(small[:, :, t % 4])), t
+    Q = torch.randn((B, Hkv, D), generator=_gen(2)).bfloat16().cuda()
+    s, want = hb.query_scores(sh, Q, bounds, kv.k_map), hb.query_scores(few_shape, Q, small)
+    assert torch.equal(s, want.repeat(1, 1, T // 4))
+    best = hb.pick_tiles(sh, s, 3)
+    assert torch.equal(best, (want.argmax(-1, keepdim=True) + 4 * torch.arange(3, device="cuda")).int())
+
+
+@gpu
+@pytest.mark.parametrize("Lq", [1, 301])
+def test_listed_attention_in_pools_beyond_32_bits(Lq):
+    """Slots behind 4 GiB of either pool."""
+    T, cap = 8, 600000
+    sh = hb.make_shape(1, 4, 1, T * TILE)
+    K = torch.randn((1, 1, T * TILE, D), generator=_gen(1)).bfloat16().cuda()
+    near = hb.compress_kv(sh, hb.make_policy(), K, K)
+    far = hb.PackedKV(sh, [0, 0, cap, 0, cap], "cuda")
+    far.uniform = 0
+    for name, size in (("k_nnz", 8192), ("k_meta", 1024), ("v_nnz", 8192), ("v_meta", 1024)):
+        getattr(far, name)[-T * size:] = getattr(near, name)
+    far.k_map, far.v_map = near.k_map - (cap - T), near.v_map - (cap - T)
+    Q = torch.randn((1, 4, Lq, D), generator=_gen(2)).bfloat16().cuda()
+    lists = torch.tensor([1, 4, 7], dtype=torch.int32, device="cuda").expand(1, 1, Lq, 3).contiguous()
+    near.uniform = 0
+    for a, b in zip(hb.listed_attn(sh, Q, far, lists, causal=False), hb.listed_attn(sh, Q, near, lists, causal=False)):
+        assert torch.equal(a, b)
+    assert torch.equal(_bits(hb.tile_bounds(sh, far)), _bits(hb.tile_bounds(sh, near)))
 
 
 @gpu
