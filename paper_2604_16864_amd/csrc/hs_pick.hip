@@ -49,6 +49,7 @@ __device__ __forceinline__ float wave_max_63(float x) {
   return x;
 }
 
+// What bounds all of this is latency: a row is a few kilobytes, read once, and a chain of steps that each wait for the one before.
 // One workgroup per query.  A thread has PER scores, of tiles j NT + tid, in registers (of long rows it reads them anew for each pass); a wave's 64 are one
 // word of the row's bits.  Tiles that are open (score above -inf) are numbered to find the ends.  The others are counted into bins of equal width between the
 // largest and the smallest finite score; the bins above the one in which the count is reached are in, and of that one those with the best ranks (score
@@ -200,16 +201,98 @@ __global__ __launch_bounds__(NT) void pick_kernel(int T, const float* __restrict
   for (int i = number.total + tid; i < n_pick; i += NT) out[i] = -1;
 }
 
+// Rows of few tiles: a wave per row, 64 PER tiles, nothing shared.  The bound is found bit by bit from the highest one that two ranked scores differ in: how
+// many have a 0 there, by ballots; until a half is taken whole.
+template <int PER>
+__global__ __launch_bounds__(256) void pick_wave_kernel(int64_t rows, int T, const float* __restrict__ scores, int n_pick, int first, int last, int32_t* __restrict__ list) {
+  const int l = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (r >= rows) return;
+  const float* row = scores + r * T;
+  int32_t* out = list + r * n_pick;
+  uint32_t key[PER];  // rises where the score falls
+  unsigned long long in[PER];
+  int n_open = 0;
+#pragma unroll
+  for (int j = 0; j < PER; j++) {
+    const int t = 64 * j + l;
+    const float x = t < T ? row[t] : -INFINITY;
+    key[j] = ~rank_key(x == x ? x : INFINITY);  // NaN: a tile that cannot be ruled out
+    in[j] = __ballot(!(x == -INFINITY));
+    n_open += __builtin_popcountll(in[j]);
+  }
+  if (n_open > n_pick) {
+    const int n_first = min(first, n_open), n_last = min(last, n_open - n_first);
+    int rest = n_pick - n_first - n_last;
+    unsigned long long ranked[PER];
+    uint32_t any = 0u, all = ~0u;
+    int before = 0;
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+      const int at = before + bits_below(in[j], l);
+      const bool mine = (in[j] >> l & 1ull) && at >= n_first && at < n_open - n_last;
+      ranked[j] = __ballot(mine);
+      before += __builtin_popcountll(in[j]);
+      any |= mine ? key[j] : 0u;
+      all &= mine ? key[j] : ~0u;
+    }
+    const uint64_t both = wave_or((uint64_t)any << 32 | (uint32_t)~all);
+    any = (uint32_t)(both >> 32);
+    all = ~(uint32_t)both;
+    // keys from low on, span + 1 of them: those that the bound is among; rest: how many of them are taken.  All before low are.
+    const uint32_t differ = any ^ all;
+    const int bits = differ != 0u ? 32 - __builtin_clz(differ) : 0;
+    uint32_t span = bits == 32 ? ~0u : (1u << bits) - 1u, low = all & ~span;
+    bool whole = rest == 0;  // of those: all, or (rest == 0) none
+    for (int b = bits - 1; b >= 0 && !whole; b--) {
+      span >>= 1;
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < PER; j++) n += __builtin_popcountll(__ballot(key[j] - low <= span) & ranked[j]);
+      if (n < rest) {
+        rest -= n;
+        low += span + 1u;
+      } else {
+        whole = n == rest;
+      }
+    }
+    int same = 0;
+#pragma unroll
+    for (int j = 0; j < PER; j++) {
+      const unsigned long long level = __ballot(key[j] >= low && key[j] - low <= span) & ranked[j], better = __ballot(key[j] < low) & ranked[j];
+      const unsigned long long taken = __ballot((level >> l & 1ull) && same + bits_below(level, l) < rest);
+      same += __builtin_popcountll(level);
+      in[j] = (in[j] & ~ranked[j]) | (n_pick - n_first - n_last > 0 ? better | taken : 0ull);
+    }
+  }
+  int number = 0;
+#pragma unroll
+  for (int j = 0; j < PER; j++) {
+    if (in[j] >> l & 1ull) out[number + bits_below(in[j], l)] = 64 * j + l;
+    number += __builtin_popcountll(in[j]);
+  }
+  for (int i = number + l; i < n_pick; i += 64) out[i] = -1;
+}
+
 }  // namespace
 
 // Threads of a row: many hide the latency of the steps where rows are few, few leave more rows side by side.  us a call, replayed from a graph, 32 tiles of
 // T picked, 256 / 512 / 1024 threads:
 //   8 rows     T = 512   3.9 / 3.6 / 4.1    1000   4.9 / 4.1 / 4.3    2048   6.9 / 5.2 / 5.1    4096     - / 7.3 / 6.4
 //   1024 rows  T = 512   5.1 / 5.9 / 12.3   1000   6.7 / 7.4 / 13.8   2048   9.4 / 10.0 / 16.8  4096     - / 16.6 / 23.3
+// a workgroup / a wave for each:
+//   8 rows     T = 64    3.3 / 2.9          128    3.3 / 3.6          200    3.4 / 4.2
+//   2048 rows  T = 64    5.3 / 4.1          128    5.5 / 4.7          200    5.8 / 6.4
+//   8192 rows  T = 64    12.6 / 6.7         128    13.6 / 8.5         200    14.5 / 11.2          512  19.5 / 20.9
 hipError_t hs_launch_pick(int64_t rows, int T, const float* scores, int n_pick, int first, int last, int32_t* list, hipStream_t st) {
 #define HS_PICK(NT_, PER_) hipLaunchKernelGGL((pick_kernel<NT_, PER_>), dim3((unsigned)rows), dim3(NT_), 0, st, T, scores, n_pick, first, last, list)
+#define HS_PICK_WAVE(PER_) \
+  hipLaunchKernelGGL((pick_wave_kernel<PER_>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, rows, T, scores, n_pick, first, last, list)
   const bool few = rows <= 512;
-  if (T <= 256) HS_PICK(256, 1);
+  if (T <= 64) HS_PICK_WAVE(1);
+  else if (T <= 128 && rows > 1024) HS_PICK_WAVE(2);
+  else if (T <= 256 && rows > 4096) HS_PICK_WAVE(4);
+  else if (T <= 256) HS_PICK(256, 1);
   else if (T <= 512) { if (few) HS_PICK(512, 1); else HS_PICK(256, 2); }
   else if (T <= 1024) { if (few) HS_PICK(512, 2); else HS_PICK(256, 4); }
   else if (T <= 2048) HS_PICK(512, 4);
@@ -218,5 +301,6 @@ hipError_t hs_launch_pick(int64_t rows, int T, const float* scores, int n_pick, 
   else if (T <= 16384) HS_PICK(1024, 16);
   else HS_PICK(1024, 64);
 #undef HS_PICK
+#undef HS_PICK_WAVE
   return hipGetLastError();
 }

@@ -203,20 +203,21 @@ def test_pick(T, Lq):
 
 
 @gpu
-@pytest.mark.parametrize("T", [90, 300, 700, 1500, 3000])
-def test_pick_for_many_queries(T):
-    """More than 512 rows, which other numbers of threads take."""
+@pytest.mark.parametrize("T,Lq", [(90, 190), (300, 190), (700, 190), (1500, 190), (3000, 190), (1, 400), (64, 400), (65, 400), (128, 400), (129, 1400), (256, 1400)])
+def test_pick_for_many_queries(T, Lq):
+    """More than 512, 1024 and 4096 rows, which other numbers of threads take."""
     g = _gen(T)
     sh = hb.make_shape(1, 3, 3, T * TILE)
-    s = (torch.randn((1, 3, 190, T), generator=g) * 4).half().float()
+    s = (torch.randn((1, 3, Lq, T), generator=g) * 4).half().float()
+    s[0, 0, 0, ::3], s[0, 0, 1, ::2], s[0, 0, 2], s[0, 0, 3], s[0, 0, 4] = math.nan, math.inf, 2.5, -math.inf, torch.where(torch.rand(T, generator=g) < 0.5, 0.0, -0.0)
     s[torch.rand(s.shape, generator=g) < 0.2] = -math.inf
-    for n, first, last in ((24, 1, 4), (1, 0, 0), (T // 2, 3, 0)):
+    for n, first, last in ((24, 1, 4), (1, 0, 0), (max(3, T // 2), 3, 0), (5, 1, 4)):
         assert (hb.pick_tiles(sh, s.cuda(), n, first, last).cpu().numpy() == ref.pick_tiles(s.numpy(), n, first, last)).all(), (n, first, last)
 
 
 @gpu
 @pytest.mark.parametrize("kind", ["alike", "two values", "zeros of both signs", "special", "none", "near"])
-@pytest.mark.parametrize("T", [100, 1000, 5000, 20000])
+@pytest.mark.parametrize("T", [40, 100, 1000, 5000, 20000])
 def test_pick_of_special_scores(T, kind):
     g = _gen(T)
     s = {"alike": torch.full((1, 1, 3, T), -2.5), "two values": (torch.rand((1, 1, 3, T), generator=g) < 0.1).float(),
@@ -318,6 +319,50 @@ def test_lists_are_sets(policy, dtype):
     mixed = torch.cat([base, base[..., :7], torch.full((B, Hkv, 7), T)], -1)[..., torch.randperm(n, generator=g)].to(torch.int32)
     a, b = hb.listed_attn(sh, Q, kv, sorted_.cuda()), hb.listed_attn(sh, Q, kv, mixed.contiguous().cuda())
     assert torch.equal(_bits(a[0]), _bits(b[0])) and torch.equal(a[1], b[1])
+
+
+@gpu
+@pytest.mark.parametrize("policy", ["2:4", "dense", "dense keys", "dense values", "half"])
+@pytest.mark.parametrize("far", [(), (0,), (3, 4), (1, 5, 9), tuple(range(12))])
+@pytest.mark.parametrize("Lq", [1, 5, 310])
+def test_value_tiles_in_either_encoding(Lq, far, policy):
+    """bf16 caches whose value tiles are held in fp16 encoding, but for some of values that fp16 does not hold."""
+    def spoil(K, V):
+        for t in far:
+            V[:, :, t * TILE:(t + 1) * TILE] *= 2.0 ** -20
+    T = 12
+    sh, kv, K, V, held = _cache(1, 4, 1, T, "bf16", policy, 13, spoil)
+    assert {t for t in range(T) if not int(kv.v_map[0, 0, t].abs()) & hb.MAP_F16} >= set(far)
+    Q = torch.randn((1, 4, Lq, D), generator=_gen(2)).bfloat16()
+    lists = torch.tensor([9, 0, 3, 1, 4, 11, 5], dtype=torch.int32).expand(1, 1, Lq, 7).contiguous()
+    lists[:, :, ::2] = lists[:, :, ::2].sort(-1).values
+    want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, D ** -0.5, weight=2.0 ** (-16 if Lq <= 300 else -11))
+    o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=False)
+    _close_attention(o, lse, want, torch.bfloat16)
+
+
+@gpu
+def test_two_calls_at_once():
+    """Two streams, each with its own lists and workspace, over one cache."""
+    sh, kv, _, _, _ = _cache(2, 8, 2, 60, "bf16", "half", 23)
+    g = _gen(24)
+    Q = [torch.randn((2, 8, D), generator=g).bfloat16().cuda() for _ in range(2)]
+    bounds = hb.tile_bounds(sh, kv)
+
+    def step(q):
+        return hb.listed_attn(sh, q, kv, hb.pick_tiles(sh, hb.query_scores(sh, q, bounds, kv.k_map), 30, 1, 4))
+    want = [step(q) for q in Q]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(step(Q[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o, lse in got[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
 
 
 @gpu
