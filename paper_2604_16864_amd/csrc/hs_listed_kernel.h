@@ -40,7 +40,7 @@ constexpr int kLaneEntries = 4;  // entries of a list that a lane can hold: list
 // tiles in ascending order, its waves every fourth of these.  Which tiles these are every wave finds by itself, in registers, where the list is what
 // hs_pick_tiles writes: ascending, what is no tile (or begins behind a causal query) at its end.  Any other list is marked in a bit map of the row's tiles and
 // numbered from there, so that order, tiles named twice and numbers between them that are no tiles do not matter.
-// The tile that a causal query stands in is left out of this and done by the last workgroup's last wave, with the tokens behind the query cut off.  The dense
+// The tile that a causal query stands in is left out of this and done by the last workgroup's first wave, which has the fewest of the others, with the tokens behind the query cut off.  The dense
 // tail has workgroups of its own behind all others, or, of a query that one workgroup does, is its first four waves' beginning.
 // UNIFORM: as in decode attention, slot == tile and one kind per tensor; the K map is not read.  STREAM: tiles are read past the caches.
 template <int KM, int VM, bool F16, bool UNIFORM, int NW, bool STREAM>
@@ -248,7 +248,7 @@ void listed_kernel(hs_listed_args g, hs_kv_dev kv, int n_splits, float scale_log
       __syncthreads();  // the list is rewritten by the next pass
     }
   }
-  if (cut && last_split && w == NW - 1) {
+  if (cut && last_split && w == 0) {
     const int mk = __builtin_amdgcn_readfirstlane(kv.k_map[(int64_t)row * T + t_cut]), mv = __builtin_amdgcn_readfirstlane(kv.v_map[(int64_t)row * T + t_cut]);
     const int limit = (int)((pos + 1) % HS_BT) - 1;
     static_for_forms<KM, VM, F16, -1>([&](auto form_c) {
