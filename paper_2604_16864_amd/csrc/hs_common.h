@@ -279,7 +279,7 @@ struct hs_listed_args {
   int32_t B, Hq, Hkv, T, Lq, q_start, causal, n_list, tail_len;  // tail_len < 0: no tail
   float scale;
 };
-// shares that a list is cut into, waves of a workgroup (4, or 8 for single queries in one share), and neighbouring queries of a workgroup; with more than one share
+// shares that a list is cut into, waves of a workgroup (4, or 8 with one share), and neighbouring queries of a workgroup; with more than one share
 // their results go through ws: B * Hq * Lq * 129 floats for each, and as much for a tail.  Workgroups: B Hkv ceil(Lq / queries) splits.
 struct hs_listed_plan { int splits, waves, queries; };
 hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list);

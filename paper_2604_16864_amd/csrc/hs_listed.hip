@@ -12,6 +12,7 @@
 // A step of single tokens reads past the caches: what it reads comes again with the next step, when the other layers' have gone through them.  128 rows of 64 tiles, 151 MB
 // that are not in the last-level cache: 30.7 us, through the caches 34.9; 512 rows 94 and 108.  Queries that stand side by side pick much the same tiles, and
 // read through the caches: 65 of them with 41 tiles each on 4 rows 22.2 us, past them 29.9.
+// 256 of them with 64 each on 8 rows 20.2 with 4 waves, 17.5 with 8.
 // Neighbouring queries in one workgroup, over all tiles that one of them picks (hs_listed_many.hip), against one by one, lists that differ in a third of their tiles:
 // 32 rows 11.9 and 9.9, 128 rows 15.3 and 13.9, 256 rows 19.2 and 20.4, 320 rows 15.2 and 16.1 (dense 18.4 and 22.4; 8 heads a row, two queries a workgroup, 17.8 and
 // 16.7), 384 rows 20.6 and 25.9, 600 rows 25.7 and 38.6, 2400 rows 56.5 and 111.
@@ -25,7 +26,7 @@ hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list)
     if (p.queries > Lq) p.queries = Lq;
     rows = (int64_t)B * Hkv * (((int64_t)Lq + p.queries - 1) / p.queries);
   } else if (rows > 128 || n_list <= 8 || (rows > 64 && n_list <= 32)) {
-    if (rows <= 256 && Lq == 1) p.waves = 8;
+    if (rows <= 256) p.waves = 8;
     return p;
   }
   const int by_rows = rows > 256 ? 1 : (int)(256 / rows), by_tiles = n_list / 4 + (n_list % 4 != 0);

@@ -296,12 +296,13 @@ hipError_t launch_listed(const hs_listed_args& a, const hs_kv_dev& kv, bool f16,
   const float sl2 = a.scale * kLog2e;
 #define HS_LISTED(F16_, NW_, STREAM_) \
   hipLaunchKernelGGL((listed_kernel<KM, VM, F16_, UNIFORM, NW_, STREAM_>), grid, block, lds, st, a, kv, p.splits, sl2, wo, wl)
-#define HS_LISTED_AS(F16_) \
-  if (a.Lq > 1) HS_LISTED(F16_, 4, false); else if (p.waves == 8) HS_LISTED(F16_, 8, true); else HS_LISTED(F16_, 4, true)
+#define HS_LISTED_AS(F16_)                                                                     \
+  if (a.Lq == 1) { if (p.waves == 8) HS_LISTED(F16_, 8, true); else HS_LISTED(F16_, 4, true); } \
+  else { if (p.waves == 8) HS_LISTED(F16_, 8, false); else HS_LISTED(F16_, 4, false); }
   if (f16) {
-    HS_LISTED_AS(true);
+    HS_LISTED_AS(true)
   } else {
-    HS_LISTED_AS(false);
+    HS_LISTED_AS(false)
   }
 #undef HS_LISTED_AS
 #undef HS_LISTED
