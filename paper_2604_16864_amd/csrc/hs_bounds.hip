@@ -4,6 +4,12 @@
 namespace {
 
 typedef short s16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// read past the caches: what is read once a call
+__device__ __forceinline__ uint4 ld_past(const uint4* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
+}
 
 // Two 16-bit floating-point numbers as integers of the same order: -NaN < -inf < .. < -0 < +0 < .. < inf < +NaN.  Its own inverse.
 __device__ __forceinline__ uint32_t order_of(uint32_t x) {
@@ -34,16 +40,15 @@ __device__ __forceinline__ void halve(uint32_t* x, bool bit) {
   }
 }
 
-// A wave per tile.  What bounds it: the load stream (32768 dense tiles 98 us, 5.6 TB/s; 4096 2:4 tiles of 38 MB 9.1 us with the launch); of a 2:4 tile it issues some 740 vector
+// A wave per tile.  What bounds it: the load stream, past the caches in workgroups of one wave (32768 dense tiles 89.6 us, 6.2 TB/s; through them in workgroups of four 98.4; 4096 2:4 tiles of 38 MB
+// 10.2 and 11.5); of a 2:4 tile it issues some 740 vector
 // instructions, 2900 clocks of a SIMD where the stream leaves it 4000.  Its keys are read in the pool's order: lane (a, r) holds tokens 16 m + r and 32 channels of each, as 16 pairs, over which it
 // keeps the lowest and the highest; then the 16 lanes of a hand each other halves of them (lowest and inverted highest: 32 words), until each has
 // 4 channels of one bound.
-__global__ __launch_bounds__(64 * HS_BOUNDS_TILES) void bounds_kernel(hs_kv_dev kv, int n_rows, int Hkv, int T, int tile, int n_tiles,
-                                                                      const int32_t* __restrict__ tiles, uint16_t* __restrict__ bounds) {
-  const int l = threadIdx.x & 63, a = l >> 4, r = l & 15;
-  const int n = blockIdx.x * HS_BOUNDS_TILES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = n / n_tiles;
-  if (row >= n_rows) return;
+__global__ __launch_bounds__(64) void bounds_kernel(hs_kv_dev kv, int Hkv, int T, int tile, int n_tiles, const int32_t* __restrict__ tiles,
+                                                    uint16_t* __restrict__ bounds) {
+  const int l = threadIdx.x, a = l >> 4, r = l & 15;
+  const int n = blockIdx.x, row = n / n_tiles;
   int t = tile + (n - row * n_tiles);
   if (tiles != nullptr) {
     t = tiles[row / Hkv];
@@ -65,7 +70,7 @@ __global__ __launch_bounds__(64 * HS_BOUNDS_TILES) void bounds_kernel(hs_kv_dev 
     for (int m = 0; m < 4; m++)
 #pragma unroll
       for (int s = 0; s < 4; s++) {
-        const uint4 v = p[64 * (4 * m + s)];
+        const uint4 v = ld_past(p + 64 * (4 * m + s));
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
@@ -78,13 +83,13 @@ __global__ __launch_bounds__(64 * HS_BOUNDS_TILES) void bounds_kernel(hs_kv_dev 
   } else {
     const int64_t slot = (int64_t)row * kv.cap_sparse_k + (-mk - 1);
     const uint4* p = reinterpret_cast<const uint4*>(kv.k_nnz + slot * HS_TILE_NNZ_BYTES) + l;
-    const uint4 at = reinterpret_cast<const uint4*>(kv.k_meta + slot * HS_TILE_META_BYTES)[l];
+    const uint4 at = ld_past(reinterpret_cast<const uint4*>(kv.k_meta + slot * HS_TILE_META_BYTES) + l);
     const uint32_t idx[4] = {at.x, at.y, at.z, at.w};
 #pragma unroll
     for (int m = 0; m < 4; m++)
 #pragma unroll
       for (int kb = 0; kb < 2; kb++) {
-        const uint4 v = p[64 * (2 * m + kb)];
+        const uint4 v = ld_past(p + 64 * (2 * m + kb));
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int q = 0; q < 4; q++) {
@@ -173,8 +178,9 @@ __device__ __forceinline__ void store_scores(const hs_scores_args& g, int row, i
 }
 __device__ __forceinline__ bool wide_scores(const hs_scores_args& g) { return (g.T & 3) == 0 && ((uintptr_t)g.scores & 15) == 0; }
 
-// One query per sequence.  What bounds it: reading the bounds, 256 rows of 2048 tiles of which a quarter is SKIP 41 us, 5.0 TB/s (one block of 16 tiles a wave 46; SKIP tiles read too 58).
-// grid = (tiles, rows); a wave has n_blocks <= 4 blocks of 16 tiles, the next one requested while one is multiplied.  Columns are the
+// One query per sequence.  What bounds it: reading the bounds, 256 rows of 2048 tiles of which a quarter is SKIP 38 to 40 us, 5.2 TB/s (SKIP tiles read too 58); all of them held 48, 5.6 TB/s; 512 rows 91, 5.9 TB/s.
+// Reads past the caches are no faster here (52, 100).
+// grid = (tiles, rows); a wave has n_blocks (1 or 2) blocks of 16 tiles, both requested at once.  Columns are the
 // group's heads, over again up to 16.
 template <bool F16>
 __global__ __launch_bounds__(256) void scores_one_kernel(hs_scores_args g, int n_blocks) {
@@ -203,16 +209,11 @@ __global__ __launch_bounds__(256) void scores_one_kernel(hs_scores_args g, int n
     }
     if (c == 0) store_scores(g, row, 0, t0 + 16 * k + 4 * a, s, held, wide);
   };
-  TileBounds even, odd;
-  load(even, 0);
-  for (int k = 0; k < n_blocks; k += 2) {  // blocks behind the row have no held tile and are not stored
-    if (k + 1 < n_blocks) load(odd, k + 1);
-    use(even, k);
-    if (k + 1 < n_blocks) {
-      if (k + 2 < n_blocks) load(even, k + 2);
-      use(odd, k + 1);
-    }
-  }
+  TileBounds first, second;
+  load(first, 0);
+  if (n_blocks > 1) load(second, 1);  // a block behind the row has no held tile and is not stored
+  use(first, 0);
+  if (n_blocks > 1) use(second, 1);
 }
 
 // More queries.  What bounds it: latency while queries are few (65 queries, 7 heads, 777 tiles, 4 rows: 6.3 us); heads known to the compiler are worth 0.6 of it, their products side by side.
@@ -254,8 +255,7 @@ __global__ __launch_bounds__(256) void scores_kernel(hs_scores_args g, int per_r
 
 hipError_t hs_launch_bounds(int B, int Hkv, int T, const hs_kv_dev& kv, int tile, int n_tiles, const int32_t* tiles, uint16_t* bounds, hipStream_t st) {
   const int64_t n = (int64_t)B * Hkv * n_tiles;
-  hipLaunchKernelGGL(bounds_kernel, dim3((unsigned)((n + HS_BOUNDS_TILES - 1) / HS_BOUNDS_TILES)), dim3(64 * HS_BOUNDS_TILES), 0, st, kv, B * Hkv, Hkv, T,
-                     tile, n_tiles, tiles, bounds);
+  hipLaunchKernelGGL(bounds_kernel, dim3((unsigned)n), dim3(64), 0, st, kv, Hkv, T, tile, n_tiles, tiles, bounds);
   return hipGetLastError();
 }
 
@@ -263,7 +263,8 @@ hipError_t hs_launch_scores(const hs_scores_args& a, int dtype, hipStream_t st) 
   const int rows = a.B * a.Hkv, tile_blocks = (a.T + 15) / 16;
   const int64_t fixed = (int64_t)rows * tile_blocks;
   if (a.Lq == 1) {
-    const int n = fixed >= 16384 ? 4 : (fixed >= 8192 ? 2 : 1);  // blocks of a wave
+    // blocks of a wave, us: 512 rows of 2048 tiles, 1: 93.9, 2: 91.6, 4: 97.0; 128 rows of 512, 9.5, 8.9, 10.0; 8 rows of 512, 3.0, 3.6, 4.9
+    const int n = fixed >= 2048 ? 2 : 1;
     const int64_t per_row = (tile_blocks + n - 1) / n;
     const int waves = per_row * rows <= 1024 ? 1 : 4;
     const dim3 grid((unsigned)((per_row + waves - 1) / waves), (unsigned)rows), block(64 * waves);
