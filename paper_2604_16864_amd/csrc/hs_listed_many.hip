@@ -4,8 +4,8 @@
 
 namespace {
 // Queries that stand side by side pick much the same tiles: up to 16 / G of them share a workgroup, their heads as the 16 columns of the products, over all tiles that
-// one of their lists names.  A column whose query does not see a tile, or not all of it, has scores of -inf there.  What bounds it: per tile the vector ALU
-// (the exponentials of 16 columns) and the reads from the L2 alike.
+// one of their lists names.  A column whose query does not see a tile, or not all of it, has scores of -inf there.  What bounds it: a tile's chain of loads,
+// products, exponentials and products with two waves a SIMD, 0.5 us a tile and wave (2400 queries of 64 tiles, 4 heads, 56 us; three waves a SIMD spill, 73).
 // The numerators enter the second product in one term of 11 bits (a V tile in fp16 encoding), or two of 8 (bf16).
 template <int KM, int VM, bool F16, int ENC, typename Limit>
 __device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, const uint4 (&qb)[4], float scale_log2, f32x4_t (&o)[8], float& m_run, float& l_run,
@@ -37,9 +37,15 @@ __device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, con
     for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[m][i]);
   mx = fmaxf(mx, __shfl_xor(mx, 16));
   mx = fmaxf(mx, __shfl_xor(mx, 32));
-  m_run = fmaxf(m_prev, mx * scale_log2 - kShift);
+  // The reference follows the maximum only when that has grown by more than kSlack binades (numerators then reach 2^15, which fp16 holds): a row's tiles mostly leave it, and
+  // the accumulators, as they are.
+  constexpr float kSlack = 7.f;
+  const float want = mx * scale_log2 - kShift;
+  float alpha = 1.f;
+  const bool moves = __ballot(want > m_prev + kSlack) != 0ull;
+  if (moves) m_run = fmaxf(m_prev, want);
   const float m_ref = m_run > -INFINITY ? m_run : 0.f;  // nothing seen so far: weights 0, not exp2(-inf + inf)
-  const float alpha = __builtin_amdgcn_exp2f(m_prev - m_ref);
+  if (moves) alpha = __builtin_amdgcn_exp2f(m_prev - m_ref);
   float p[4][4], psum = 0.f;
 #pragma unroll
   for (int m = 0; m < 4; m++)
@@ -49,8 +55,10 @@ __device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, con
       psum += p[m][i];
     }
   l_run = l_run * alpha + psum;
+  if (moves) {
 #pragma unroll
-  for (int i = 0; i < 8; i++) o[i] *= alpha;
+    for (int i = 0; i < 8; i++) o[i] *= alpha;
+  }
   uint32_t hi[8];
 #pragma unroll
   for (int m = 0; m < 4; m++) {
