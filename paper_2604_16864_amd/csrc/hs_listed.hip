@@ -15,7 +15,7 @@
 // 256 of them with 64 each on 8 rows 20.2 with 4 waves, 17.5 with 8.
 // Neighbouring queries in one workgroup, over all tiles that one of them picks (hs_listed_many.hip), against one by one, lists that differ in a third of their tiles:
 // 32 rows 11.9 and 9.9, 128 rows 15.3 and 13.9, 256 rows 19.2 and 20.4, 320 rows 15.2 and 16.1 (dense 18.4 and 22.4; 8 heads a row, two queries a workgroup, 17.8 and
-// 16.7), 384 rows 20.6 and 25.9, 600 rows 25.7 and 38.6, 2400 rows 56.5 and 111.
+// 16.7), 384 rows 20.6 and 25.9, 600 rows 25.7 and 38.6, 2400 rows 56.0 and 111.
 hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list) {
   hs_listed_plan p{1, 4, 1};
   int64_t rows = (int64_t)B * Hkv * Lq;
