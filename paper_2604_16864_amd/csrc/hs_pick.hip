@@ -1,4 +1,6 @@
 // Choice of the tiles that a query attends to, by their scores.
+#include <limits.h>
+
 #include "hs_rank.h"
 
 namespace {
@@ -134,7 +136,8 @@ __global__ __launch_bounds__(NT) void pick_kernel(int T, const float* __restrict
       return at < (float)(kBins - 1) ? (int)at : kBins - 1;
     };
     auto rank = [&](int j, float x) { return rank_of(~rank_key(x), j * NT + tid); };
-    int bound_bin = 0, left = rest, in_bin = kListed + 1;  // not binned: all are in the bin that is looked at
+    // not binned: all that are ranked are in question, more of them than are left to take, and compared by radix selection whatever their number
+    int bound_bin = 0, left = rest, in_bin = INT_MAX;
     if (binned) {
       each([&](int j, float x) { if (ranked >> j & 1ull) atomicAdd(&hist[bin_of(x)], 1); });
       __syncthreads();

@@ -233,6 +233,40 @@ def test_pick_of_special_scores(T, kind):
         assert (hb.pick_tiles(sh, s.cuda(), n, first, last).cpu().numpy() == ref.pick_tiles(s.numpy(), n, first, last)).all(), (n, first, last)
 
 
+def _unranked(kind, T, g):
+    """Three rows of scores whose finite ones span no width that 32 bits hold, or that have none."""
+    s = torch.full((3, T), {"nan": math.nan}.get(kind, math.inf))
+    if kind == "inf and nan":
+        s[torch.rand((3, T), generator=g) < 0.5] = math.nan
+    elif kind == "wide":
+        s = (torch.rand((3, T), generator=g) * 2 - 1) * 3.4e38
+        s[:, 7], s[:, 11] = -3.4e38, 3.4e38
+    elif kind == "alike":
+        s[:] = 1.5
+    s[1, torch.rand(T, generator=g) < 0.1] = -math.inf
+    return s
+
+
+@gpu
+@pytest.mark.parametrize("first,last", [(0, 0), (1, 4)])
+@pytest.mark.parametrize("kind", ["inf", "nan", "inf and nan", "wide", "alike"])
+@pytest.mark.parametrize("T", [72, 100, 300, 600, 1000, 2000, 4000, 5000, 10000, 20000])
+def test_pick_of_scores_without_a_width(T, kind, first, last):
+    """Any number left to take by score, those about the most that are ranked one against all (64) among them; nothing is written behind the lists."""
+    rows = _unranked(kind, T, _gen(T))
+    for Lq in (3, 600):
+        sh = hb.make_shape(1, 1, 1, T * TILE)
+        s = rows.repeat(Lq // 3, 1)[None, None].contiguous().cuda()
+        for rest in sorted({1, 2, 63, 64, 65, 66, 67, 128, 129, T // 2}):
+            n = rest + first + last
+            space = torch.full((Lq * n + 2 * T + 128,), 77, dtype=torch.int32, device="cuda")
+            out = space[64:64 + Lq * n].view(1, 1, Lq, n)
+            got = hb.pick_tiles(sh, s, n, first, last, out=out).cpu().numpy()[0, 0]
+            want = ref.pick_tiles(rows.numpy(), n, first, last)
+            assert (got.reshape(-1, 3, n) == want).all(), (Lq, rest)
+            assert bool((space[:64] == 77).all()) and bool((space[64 + Lq * n:] == 77).all()), (Lq, rest)
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # attention over listed tiles
 # ---------------------------------------------------------------------------------------------------------------------
