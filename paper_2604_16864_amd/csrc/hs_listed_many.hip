@@ -7,9 +7,10 @@ namespace {
 // one of their lists names.  A column whose query does not see a tile, or not all of it, has scores of -inf there.  What bounds it: a tile's chain of loads,
 // products, exponentials and products with two waves a SIMD, 0.5 us a tile and wave (2400 queries of 64 tiles, 4 heads, 56 us; three waves a SIMD spill, 73).
 // The numerators enter the second product in one term of 11 bits (a V tile in fp16 encoding), or two of 8 (bf16).
+constexpr float kSlack = 7.f;  // numerators reach 2^15, which fp16 holds
 template <int KM, int VM, bool F16, int ENC, typename Limit>
-__device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, const uint4 (&qb)[4], float scale_log2, f32x4_t (&o)[8], float& m_run, float& l_run,
-                                                  Limit limit) {
+__device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, const uint4 (&qb)[4], float scale_log2, float slack, f32x4_t (&o)[8], float& m_run,
+                                                  float& l_run, Limit limit) {
   constexpr int kNK = TileRegs<KM, VM>::kNK, kNV = TileRegs<KM, VM>::kNV;
   typedef hs_elem<F16> E;
   typedef hs_elem<ENC == 1> EV;
@@ -37,12 +38,10 @@ __device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, con
     for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[m][i]);
   mx = fmaxf(mx, __shfl_xor(mx, 16));
   mx = fmaxf(mx, __shfl_xor(mx, 32));
-  // The reference follows the maximum only when that has grown by more than kSlack binades (numerators then reach 2^15, which fp16 holds): a row's tiles mostly leave it, and
-  // the accumulators, as they are.
-  constexpr float kSlack = 7.f;
+  // The reference follows the maximum only when that has grown by more than `slack` binades: a row's tiles mostly leave it, and the accumulators, as they are.
   const float want = mx * scale_log2 - kShift;
   float alpha = 1.f;
-  const bool moves = __ballot(want > m_prev + kSlack) != 0ull;
+  const bool moves = __ballot(want > m_prev + slack) != 0ull;
   if (moves) m_run = fmaxf(m_prev, want);
   const float m_ref = m_run > -INFINITY ? m_run : 0.f;  // nothing seen so far: weights 0, not exp2(-inf + inf)
   if (moves) alpha = __builtin_amdgcn_exp2f(m_prev - m_ref);
@@ -93,7 +92,8 @@ __device__ __forceinline__ void tile_compute_many(const TileRegs<KM, VM>& r, con
 // then has its tiles).  The lists are marked in a bit map of the row's tiles for each query and the tiles that one names are numbered: order,
 // tiles named twice and numbers that are no tiles do not matter.
 // A product with a numerator of 0 is NaN where the value is an infinity or NaN.  So where the accumulators end up with any, which is rare, the work is done again query by
-// query, each over its own tiles alone and with the values behind it cut off.
+// query, each over its own tiles alone and with the values behind it cut off.  Finite values near the end of bf16's range get there too, their sums times 2^15; the reference
+// follows the maximum then, so that weights end at 2^8 and what single queries hold is held here.
 template <int KM, int VM, bool F16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void listed_many_kernel(hs_listed_args g, hs_kv_dev kv, int n_queries, int n_splits, float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_l) {
@@ -180,6 +180,7 @@ void listed_many_kernel(hs_listed_args g, hs_kv_dev kv, int n_queries, int n_spl
     for (int i = 0; i < 8; i++) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     m_run = -INFINITY;
     l_run = 0.f;
+    const float slack = alone < 0 ? kSlack : 0.f;
     const uint32_t active = alone < 0 ? (1u << n_here) - 1u : 1u << alone;
     const int sees_first = sees(alone < 0 ? 0 : alone);  // the least of those
     for (int r0 = lo; r0 < hi; r0 += kListCap) {         // the same trips in every thread
@@ -233,7 +234,7 @@ void listed_many_kernel(hs_listed_args g, hs_kv_dev kv, int n_queries, int n_spl
             if (alone >= 0 && !whole) cut_values<KK, VK>(tile, sees_first - t * HS_BT, a);
             more = act != 0ull;
             if (more) next();
-            tile_compute_many<KK, VK, F16, kEnc>(tile, qb, scale_log2, o, m_run, l_run, [&](f32x4_t (&s)[4]) {
+            tile_compute_many<KK, VK, F16, kEnc>(tile, qb, scale_log2, slack, o, m_run, l_run, [&](f32x4_t (&s)[4]) {
               if (more) tile_load<KK, VK, 1, false>(tile, kv, row, mk, mv, l);
               if (whole) return;
 #pragma unroll

@@ -457,6 +457,26 @@ def test_tiles_of_neighbouring_queries_do_not_touch_results(bad, policy, G):
 
 
 @gpu
+@pytest.mark.parametrize("policy", ["dense", "dense keys"])
+@pytest.mark.parametrize("Lq", [30, 320])
+def test_large_values(Lq, policy):
+    """Values whose weighted sums stay below 2^128 where no weight passes 2^8, and do not where weights reach 2^15: tiles 4 to 11 score some 6.2 binades more than
+    the first four, which those of a wave begin with."""
+    T, B, Hkv, G = 12, 1, 4, 4
+
+    def spoil(K, V):
+        K.mul_(0.2)
+        K[:, :, 4 * TILE:] += 0.38             # 128 channels and queries of about 1, a scale of 128 ** -0.5: 4.3 more
+        V.copy_((1.0 + 0.3 * V.float().abs()) * 2.0 ** 109)
+    sh, kv, K, V, held = _cache(B, G * Hkv, Hkv, T, "bf16", policy, 41, spoil)
+    Q = (1.0 + 0.1 * torch.randn((B, G * Hkv, Lq, D), generator=_gen(42))).bfloat16()
+    lists = torch.arange(T, dtype=torch.int32).expand(B, Hkv, Lq, T).contiguous()
+    want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, D ** -0.5)
+    o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=False)
+    _close_attention(o, lse, want, torch.bfloat16)
+
+
+@gpu
 @pytest.mark.parametrize("T,n", [(3000, 40), (9000, 9), (65536, 5)])
 def test_many_queries_on_long_rows(T, n):
     """Rows of more tiles than the bit maps of 16 queries hold: against single queries, whose lists they are."""
