@@ -477,6 +477,31 @@ def test_large_values(Lq, policy):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("policy", ["2:4", "dense", "half"])
+@pytest.mark.parametrize("G,Hkv,Lq", [(1, 16, 133), (3, 8, 82), (4, 8, 66), (8, 4, 66)])
+def test_steep_scores(G, Hkv, Lq, policy, dtype):
+    """Scores that rise and fall by a hundred binades from tile to tile, by few for some queries and by many for others, several tiles a wave: the running reference
+    moves often, for columns that do not see the tile too, and lags behind by up to 7 binades."""
+    T, n = 16, 9
+    sizes = torch.tensor([0.05, 0.3, 0.8, 2.0, 4.0, 1.0, 0.1, 6.0, 0.5, 3.0, 0.2, 8.0, 0.02, 5.0, 7.0, 1.5])
+
+    def spoil(K, V):
+        K.mul_(sizes.repeat_interleave(TILE)[:, None].to(K.dtype))
+    sh, kv, K, V, held = _cache(1, G * Hkv, Hkv, T, dtype, policy, 51, spoil)
+    g = _gen(52)
+    Q = (torch.randn((1, G * Hkv, Lq, D), generator=g) * torch.exp(torch.rand((1, G * Hkv, Lq, 1), generator=g) * 3.4 - 2.3)).to(TYPES[dtype])
+    lists = torch.rand((1, Hkv, Lq, T), generator=g).argsort(-1)[..., :n].to(torch.int32).contiguous()
+    for causal in (False, True):
+        pos = T * TILE - Lq + np.arange(Lq) if causal else None
+        want = ref.listed_attention(_f64(Q), _f64(K), _f64(V), lists.numpy(), held, D ** -0.5, pos, weight=2.0 ** -11)
+        # weights below the normal numbers of fp16 are off by half a step of 2^-24, the largest one is 2^8 at least
+        want[2][:] += 64 * n * 2.0 ** -33 * np.abs(_f64(V)).max()
+        o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=causal)
+        _close_attention(o, lse, want, TYPES[dtype], causal)
+
+
+@gpu
 @pytest.mark.parametrize("T,n", [(3000, 40), (9000, 9), (65536, 5)])
 def test_many_queries_on_long_rows(T, n):
     """Rows of more tiles than the bit maps of 16 queries hold: against single queries, whose lists they are."""
@@ -543,6 +568,80 @@ def _repeated(sh, small, T):
     at = torch.arange(T, dtype=torch.int32, device="cuda") % 4
     kv.k_map, kv.v_map = (m[:, :, :1].repeat(1, 1, T) - at for m in (small.k_map, small.v_map))
     return kv
+
+
+def _attention_over_copies(Q, K, V, lists, scale, weight):
+    """Attention of Q [B, Hq, Lq, D] over a cache whose tile t holds what tile t % 4 of K, V [B, Hkv, 256, D] holds, in 64 bits: a token of the four stands for as many
+    as the list has copies of its tile.  O, LSE and bounds on their error as in the oracle."""
+    B, Hq, Lq, _ = Q.shape
+    H = K.shape[1]
+    O, LSE, o_tol, l_tol = np.zeros(Q.shape), np.zeros(Q.shape[:3]), np.zeros(Q.shape), np.zeros(Q.shape[:3])
+    e = 2.0 ** -24
+    for b in range(B):
+        for hq in range(Hq):
+            h = hq // (Hq // H)
+            copies = np.stack([np.bincount(np.unique(x) % 4, minlength=4) for x in lists[b, h]]).repeat(TILE, axis=-1)
+            k, v = np.where(copies.any(0)[:, None], K[b, h], 0.0), np.where(copies.any(0)[:, None], V[b, h], 0.0)
+            s = np.where(copies > 0, scale * (Q[b, hq] @ k.T), -np.inf)
+            m = s.max(-1, keepdims=True)
+            p = copies * np.exp(s - m)
+            total, count = p.sum(-1, keepdims=True), copies.sum(-1)
+            O[b, hq], LSE[b, hq] = p @ v / total, (m + np.log(total))[:, 0]
+            off = scale * 2 * D * e * (np.abs(Q[b, hq]) @ np.abs(k).T).max(-1) + 4 * e * np.where(copies > 0, np.abs(s), 0.0).max(-1) * 1.5
+            o_tol[b, hq] = p @ np.abs(v) / total * (2 * off + weight + 2.0 ** -21 + 4 * count * e)[:, None]
+            l_tol[b, hq] = off + 2.0 ** -21 + 4 * e * np.abs(LSE[b, hq]) + 4 * count * e
+    return O, LSE, o_tol, l_tol
+
+
+@gpu
+@pytest.mark.parametrize("bad", [None, math.nan, math.inf])
+def test_neighbouring_queries_over_more_tiles_than_a_pass(bad):
+    """Up to 16 queries in company that list some 2200 or 2400 tiles among them, in one share: three passes of 1024.  With values that are no numbers in tiles that two of three
+    queries do not list, which are done again one by one."""
+    B, Hkv, T, Lq, n = 4, 2, 3000, 301, 300
+    g = _gen(61)
+    K, V = torch.randn((B, Hkv, 4 * TILE, D), generator=g).bfloat16(), torch.randn((B, Hkv, 4 * TILE, D), generator=g).bfloat16()
+    if bad is not None:
+        V[:, :, 3 * TILE + 5::7] = bad
+    few = hb.compress_kv(hb.make_shape(B, Hkv, Hkv, 4 * TILE), hb.make_policy(sparse_frac_k=0.0, sparse_frac_v=0.0), K.cuda(), V.cuda())
+    sh = hb.make_shape(B, Hkv, Hkv, T * TILE)
+    kv = hb.PackedKV(sh, [T - 4, 4, 0, 4, 0], "cuda")         # slots that repeat: a valid cache to read
+    kv.k_dense, kv.v_dense = few.k_dense, few.v_dense
+    kv.k_map, kv.v_map = (m.repeat(1, 1, T // 4) for m in (few.k_map, few.v_map))
+    Q = torch.randn((B, Hkv, Lq, D), generator=g).bfloat16()
+    lists = torch.randint(0, T, (B, Hkv, Lq, n), generator=g)
+    clean = np.arange(Lq) % 3 != 0 if bad is not None else np.ones(Lq, bool)
+    if bad is not None:
+        lists[:, :, clean] -= (lists[:, :, clean] % 4 == 3).long()
+    lists = lists.to(torch.int32)
+    for first in (0, 4, 32):                                  # the tiles of the first, of a middle and of a late workgroup
+        assert len(np.unique(lists[0, 0, first * 4:first * 4 + 16].numpy())) > 2 * 1024
+    assert hb.listed_attn_workspace_bytes(sh, Lq, n) == 0     # one share
+    o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda(), causal=False)
+    want = _attention_over_copies(_f64(Q[:, :, clean]), _f64(K), _f64(V), lists[:, :, clean].numpy(), D ** -0.5, 2.0 ** -11)
+    _close_attention(o[:, :, clean], lse[:, :, clean], want, torch.bfloat16)
+    if bad is not None:
+        assert not bool(torch.isfinite(o[:, :, ~clean].float()).all(-1).any())
+
+
+@gpu
+@pytest.mark.parametrize("B,n", [(200, 1100), (140, 2100), (300, 1500)])
+def test_single_queries_over_more_tiles_than_a_pass(B, n):
+    """Lists in any order of more than 1024 tiles, in one share: 8 waves, or 4."""
+    T = 2400
+    g = _gen(62)
+    K, V = torch.randn((B, 1, 4 * TILE, D), generator=g).half(), torch.randn((B, 1, 4 * TILE, D), generator=g).half()
+    small = hb.make_shape(B, 2, 1, 4 * TILE, dtype=torch.float16)
+    few = hb.compress_kv(small, hb.make_policy(), K.cuda(), V.cuda())
+    K, V = hb.unpack_kv(small, few)
+    sh = hb.make_shape(B, 2, 1, T * TILE, dtype=torch.float16)
+    kv = _repeated(sh, few, T)
+    Q = torch.randn((B, 2, D), generator=g).half()
+    lists = torch.stack([torch.randperm(T, generator=g)[:n] for _ in range(B)])[:, None].to(torch.int32).contiguous()
+    assert hb.listed_attn_workspace_bytes(sh, 1, n) == 0
+    o, lse = hb.listed_attn(sh, Q.cuda(), kv, lists.cuda())
+    want = _attention_over_copies(_f64(Q)[:, :, None], _f64(K), _f64(V), lists.numpy()[:, :, None], D ** -0.5, 2.0 ** -16)
+    _close_attention(o[:, :, None], lse[:, :, None], want, torch.float16)
 
 
 @gpu
