@@ -484,7 +484,8 @@ HS_API int hs_tile_bounds(const hs_shape* shape, int32_t tile, int32_t n_tiles, 
 
 /* What a query can score at most in a tile, for every (b, kv head), query and tile:
  *   scores = max over the group's Hq / Hkv heads of  sum over the channels c of  max(q_c, 0) largest_c + min(q_c, 0) smallest_c,
- * in units of q . k (a scale > 0 does not change the order), fp32.  NaN counts as +inf: such a tile cannot be ruled out.  -inf: tiles that are SKIP
+ * in units of q . k (a scale > 0 does not change the order), fp32.  NaN (0 times an infinity among them: a tile whose bounds are both
+ * -inf in some channel) counts as +inf: such a tile cannot be ruled out.  -inf: tiles that are SKIP
  * (k_map: the cache's K map, device int32 [B, Hkv, L / 64], 0 = SKIP; NULL: no tile is), and causal those that begin behind the query.
  *   Q       [B, Hq, Lq, D], 1 <= Lq <= 2^30; query i stands at q_start + i (0 <= q_start, q_start + Lq <= L if causal, else q_start is not looked at)
  *   scores  [B, Hkv, Lq, L / 64] contiguous
@@ -506,11 +507,13 @@ HS_API int hs_pick_tiles(const hs_shape* shape, int32_t Lq, const float* scores,
  *   tail  the dense tail of a decode step (Lq == 1, causal 0): tail_k, tail_v [B, Hkv, 64, D] contiguous or both NULL, tail_len tokens valid
  *         (tail_lens: device int32 [B] instead, clamped into 0 .. 64); it is attended to whatever the list says
  *   O     [B, Hq, Lq, D], LSE fp32 [B, Hq, Lq] or NULL, contiguous.  Nothing seen: O = 0, LSE = -inf; a score that is NaN: O = NaN, LSE = NaN.
- *         Keys and values that a query does not see do not touch its results, infinities and NaN among them.
- * scale as for hs_prefill_attn.  Of single queries the softmax numerators enter the second product in two 16-bit terms, as in decode attention; where many queries
- * share the work, in one fp16 term or, for values that fp16 does not hold, two bf16 terms, as in prefill.  L / 64 <= 65536, n_list <= 2^20,
+ *         Infinities and NaN of keys and values that a query does not see do not touch its results.
+ * scale as for hs_prefill_attn.  Of single queries the softmax numerators enter the second product in two 16-bit terms, as in decode attention.  Where Lq > 1 and
+ * B Hkv Lq > 300, neighbouring queries share the work: numerators enter in one fp16 term or, for values that fp16 does not hold, two bf16 terms, as in
+ * prefill, and the last bits of a query's results depend on the scores and lists of those that it shares with.  Sums are held in 32 bits, with
+ * numerators up to 2^8: where 2^8 times the sum of the values, each by its weight over the largest weight, is beyond 2^128, O is infinite or NaN.  L / 64 <= 65536, n_list <= 2^20,
  * B Hkv (Lq + 1) < 2^23 (HS_EUNSUPPORTED beyond).  workspace: hs_listed_attn_workspace_bytes bytes, 16-byte aligned (NULL where that is 0), not shared between two
- * calls in flight; no initial content.  Equal calls give equal bits, and so do lists that name the same tiles with the same n_list. */
+ * calls in flight; no initial content.  Equal calls give equal bits, and so do calls whose lists all name the same tiles with the same n_list. */
 HS_API int hs_listed_attn(const hs_shape* shape, int32_t Lq, int32_t q_start, float scale, int causal, const hs_view* Q, const hs_kv* kv,
                    const int32_t* list, int32_t n_list, const void* tail_k, const void* tail_v, int32_t tail_len, const int32_t* tail_lens,
                    void* O, float* LSE, void* workspace, void* stream);

@@ -41,7 +41,7 @@ __device__ __forceinline__ void halve(uint32_t* x, bool bit) {
 }
 
 // A wave per tile.  What bounds it: the load stream, past the caches in workgroups of one wave (32768 dense tiles 89.6 us, 6.2 TB/s; through them in workgroups of four 98.4; 4096 2:4 tiles of 38 MB
-// 10.2 and 11.5); of a 2:4 tile it issues some 740 vector
+// 10.2 and 11.5, on other cards 8.9 to 10.0); of a 2:4 tile it issues some 740 vector
 // instructions, 2900 clocks of a SIMD where the stream leaves it 4000.  Its keys are read in the pool's order: lane (a, r) holds tokens 16 m + r and 32 channels of each, as 16 pairs, over which it
 // keeps the lowest and the highest; then the 16 lanes of a hand each other halves of them (lowest and inverted highest: 32 words), until each has
 // 4 channels of one bound.

@@ -256,7 +256,7 @@ hipError_t hs_launch_keep(int B, int Hkv, int n, hs_vec_view K, hs_vec_view V, c
                           int keep, int first, int last, uint16_t* K_out, uint16_t* V_out, int32_t* index, void* ws, hipStream_t st);
 
 // -------- tiles picked for each query --------
-enum { HS_BOUNDS_TILES = 4 };  // a workgroup of 64 threads has a tile: B Hkv n_tiles <= HS_BOUNDS_TILES * HS_MAX_BLOCKS
+enum { HS_BOUNDS_TILES = 4 };  // HS_MAX_BLOCKS is for workgroups of 256 threads; one of 64 has a tile, so that four times as many fit: B Hkv n_tiles <= HS_BOUNDS_TILES * HS_MAX_BLOCKS
 hipError_t hs_launch_bounds(int B, int Hkv, int T, const hs_kv_dev& kv, int tile, int n_tiles, const int32_t* tiles, uint16_t* bounds, hipStream_t st);
 struct hs_scores_args {
   hs_vec_view q;

@@ -12,10 +12,17 @@
 // A step of single tokens reads past the caches: what it reads comes again with the next step, when the other layers' have gone through them.  128 rows of 64 tiles, 151 MB
 // that are not in the last-level cache: 30.7 us, through the caches 34.9; 512 rows 94 and 108.  Queries that stand side by side pick much the same tiles, and
 // read through the caches: 65 of them with 41 tiles each on 4 rows 22.2 us, past them 29.9.
-// 256 of them with 64 each on 8 rows 20.2 with 4 waves, 17.5 with 8.
-// Neighbouring queries in one workgroup, over all tiles that one of them picks (hs_listed_many.hip), against one by one, lists that differ in a third of their tiles:
-// 32 rows 11.9 and 9.9, 128 rows 15.3 and 13.9, 256 rows 19.2 and 20.4, 320 rows 15.2 and 16.1 (dense 18.4 and 22.4; 8 heads a row, two queries a workgroup, 17.8 and
-// 16.7), 384 rows 20.6 and 25.9, 600 rows 25.7 and 38.6, 2400 rows 56.0 and 111.
+// Neighbouring queries in one workgroup, over all tiles that one of them picks (hs_listed_many.hip), against one by one; 512 tiles a sequence, lists as perf/more_operators.py makes them (a
+// quarter of a list differs from the neighbour's; four list 98 tiles of 64 each among them, two 80, sixteen 130), no tail.  One by one with 4 waves / with 8 (of 32 and 128 rows: of 4 in shares) / in company:
+//   rows                           32                  128                 256                 260                 304                 384                 600                 2400
+//   64 tiles, 4 heads   2:4        18.7  10.5  12.3    19.1  15.3  14.2    18.8  15.9  16.3    23.8  28.2  18.1    25.2  28.9  17.5    25.3  29.2  20.9    38.9  43.0  28.0    112  142  62
+//                       dense      24.6  10.9  14.4    26.6  19.6  17.9    27.9  24.2  21.0    39.2  42.8  23.1    39.7  43.7  23.0    40.1  43.5  26.9    56.6  64.3  37.9    171  208  89
+//   64 tiles, 1 head    2:4        19.1  10.3  12.1    20.1  15.9  14.2    20.2  15.8  14.4    24.1  28.4  14.7    25.4  28.8  15.3    25.4  29.1  15.7    38.6  42.5  17.2    110  139  35
+//   64 tiles, 8 heads   2:4        17.9  10.8  12.6    18.4  15.1  15.1    19.3  16.5  19.0    23.9  28.3  24.2    25.2  28.9  23.5    25.5  29.5  24.1    39.5  43.3  32.8    116  145  80
+//   16 tiles, 4 heads   2:4         8.5   8.8  11.6     8.6   9.9  12.4     8.7   8.3  12.4    10.1  13.6  12.8    10.9  14.4  12.9    11.0  14.5  13.9    16.3  20.9  14.3    43   66   28
+//                       dense       9.3   8.9  12.9     9.5  10.2  13.2     9.5   9.5  13.5    13.1  16.7  14.6    13.4  17.1  14.5    13.6  17.2  15.7    19.7  25.0  17.6    51   80   36
+//   16 tiles, 8 heads   2:4         8.5   9.0  11.5     8.5  10.3  12.2     8.7   8.5  13.2    10.2  13.8  12.2    11.0  14.9  12.4    11.1  15.0  12.4    16.5  21.8  15.7    44   69   38
+// One border for all: long lists would share from about 128 rows on (260 of 64 tiles 23.8 one by one, 18.1 shared), short ones from about 500 (384 of 16 tiles 11.0, 13.9).
 hs_listed_plan hs_plan_listed(int B, int Hq, int Hkv, int T, int Lq, int n_list) {
   hs_listed_plan p{1, 4, 1};
   int64_t rows = (int64_t)B * Hkv * Lq;

@@ -37,7 +37,7 @@ __device__ __forceinline__ void cut_values(TileRegs<KM, VM>& r, int limit, int a
 constexpr int kLaneEntries = 4;  // entries of a list that a lane can hold: lists of up to 256 are looked at in registers
 
 // grid: n_splits workgroups for each query of each (batch, kv head) row, rows fastest.  A workgroup takes the share [n s / S, n (s + 1) / S) of the list's
-// tiles in ascending order, its waves every fourth of these.  Which tiles these are every wave finds by itself, in registers, where the list is what
+// tiles in ascending order, each of its NW waves every NW-th of these.  Which tiles these are every wave finds by itself, in registers, where the list is what
 // hs_pick_tiles writes: ascending, what is no tile (or begins behind a causal query) at its end.  Any other list is marked in a bit map of the row's tiles and
 // numbered from there, so that order, tiles named twice and numbers between them that are no tiles do not matter.
 // The tile that a causal query stands in is left out of this and done by the last workgroup's first wave, which has the fewest of the others, with the tokens behind the query cut off.  The dense

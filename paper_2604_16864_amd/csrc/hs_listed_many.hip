@@ -1,11 +1,13 @@
 // Attention over listed tiles of more than one query a sequence: neighbouring queries share a workgroup, over the tiles that any of them picks.
 #include "hs_listed_kernel.h"
-#include "hs_rank.h"
 
 namespace {
 // Queries that stand side by side pick much the same tiles: up to 16 / G of them share a workgroup, their heads as the 16 columns of the products, over all tiles that
 // one of their lists names.  A column whose query does not see a tile, or not all of it, has scores of -inf there.  What bounds it: a tile's chain of loads,
-// products, exponentials and products with two waves a SIMD, 0.5 us a tile and wave (2400 queries of 64 tiles, 4 heads, 56 us; three waves a SIMD spill, 73).
+// products, exponentials and products, 1.05 us a tile for a wave alone on its SIMD (600 rows of 64 tiles, 4 heads, 2:4, 28 us: 150 workgroups, 24 tiles a wave), and the places of the workgroups:
+// 2400 rows, 59 to 62 us, are 600 workgroups for 512 places (two a compute unit), 1.2 waves a SIMD on average; tiles come out of the L2 at 16 TB/s then, each for 16 columns, the vector ALU is active in 27 % of the
+// time, the matrix cores in 9 %.  Three waves a SIMD spill (2400 rows 73 where two took 56).  With two, nothing spills where K or V is all 2:4; else 4
+// (all dense) to 26 registers (both mixed) do in bf16, up to 9 in fp16: 2400 rows with half of both dense 79 us, all dense 87, in fp16 74 and 86.
 // The numerators enter the second product in one term of 11 bits (a V tile in fp16 encoding), or two of 8 (bf16).
 constexpr float kSlack = 7.f;  // numerators reach 2^15, which fp16 holds
 template <int KM, int VM, bool F16, int ENC, typename Limit>
